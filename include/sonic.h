@@ -19,6 +19,11 @@
  *                                 its Nexus KV (Sec. 3.2; the Nexus KV is kept
  *                                 for the rest of the session).
  *
+ * A compact cache may also be held in 4 bits a value (sonic_kv_compact_q4,
+ * sonic_compressed_decode_q4, sonic_cache_expand_q4), and cut down further by the
+ * attention its rows received (sonic_kv_compact_weights,
+ * sonic_compressed_decode_weighted, sonic_cache_evict).
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - Pointers marked "device" are HIP device pointers; "host" pointers are CPU
@@ -97,7 +102,11 @@ enum {
     SONIC_NEXUS_UP_TO_OWN = 1
 };
 
-/* Version of this ABI (bumped on any signature or layout change or addition). */
+/*
+ * Version of this ABI, bumped on any change of a signature, of a layout or of what a call does.
+ * Entry points added beside the others leave it as it is: a program that was built before them runs
+ * unchanged, and one that needs them finds out by their names.
+ */
 int32_t sonic_abi_version(void);
 
 /* Static text for a status code. */
@@ -429,6 +438,158 @@ int32_t sonic_nexus_extend(int32_t batch, int32_t total_new, int32_t num_q_heads
                            const int32_t *cache_row_cap, int32_t *cache_len, const void *q, const void *k,
                            const void *v, float softmax_scale, float *out, void *workspace,
                            size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* A compact cache in 4 bits                                                 */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * 4-bit rows.  Each tensor of the cache is two device arrays, indexed by the same
+ * rows as a bf16 cache:
+ *   codes   uint8 [rows][Hkv][d/2], the code of element 2i in the low half of byte i
+ *   scales  uint8 [rows][Hkv][d/32], one per block of 32 consecutive elements
+ * A code is an fp4 e2m1 number, 8 * sign + index into {0, .5, 1, 1.5, 2, 3, 4, 6}, and
+ * stands for that number times 2^(scale - 127).  A block of largest magnitude a gets
+ * the smallest e in [-127, 125] with a <= 7 * 2^e (125 if there is none), scale e + 127, and every value x of it
+ * the nearest number to x / 2^e (ties to the even index; above 6, 6).  So a value is off
+ * by at most max(2^e / 4, |x| / 5), 2^e being between a / 7 and 2 a / 7; rows rounded once
+ * and expanded round to the same codes again; and the rows take d/2 + d/32 bytes per
+ * head, 0.27 of bf16.  A block that holds an infinity or a NaN has scale 255 and is NaN
+ * throughout.
+ *
+ * A session over 4-bit rows: sonic_kv_compact_q4 after the prefill, then
+ * sonic_compressed_decode_q4 per token.  For the next-turn step, sonic_cache_expand_q4
+ * gives bf16 rows for sonic_nexus_extend, and sonic_kv_compact_q4 takes the result back:
+ * the bf16 cache as a packed batch (cu_seqlens from its row offsets and capacities), with
+ * SONIC_ROLE_HISTORY_TEXT on the rows past each length and any other role before.
+ */
+
+/*
+ * sonic_kv_compact into 4-bit rows: the kept rows of k and v (bf16), rounded as above.
+ * Arguments, outputs and errors are those of sonic_kv_compact; codes 16-byte aligned,
+ * scales 4-byte aligned.
+ */
+int32_t sonic_kv_compact_q4(int32_t batch, int32_t total_tokens, int32_t max_seqlen, int32_t num_kv_heads,
+                            int32_t head_dim, const int32_t *cu_seqlens, const uint8_t *role, const void *k,
+                            const void *v, void *k_cache, void *k_scale, void *v_cache, void *v_scale,
+                            const int64_t *cache_row_off, const int32_t *cache_row_cap, int32_t *cache_len,
+                            int32_t *keep_idx, int32_t *dev_status, void *stream);
+
+/*
+ * The bf16 values (exact) of request b's 4-bit rows row_begin[b] .. row_end[b] - 1, to rows
+ * out_row_off[b] .. of k and v.  Rows of k and v past those are left as they were.
+ *   max_rows              host bound: row_end[b] - row_begin[b] <= max_rows for every b
+ *   row_begin, row_end    device int32 [B], 0 <= row_begin[b] <= row_end[b] <= cache_row_cap[b]
+ *   k, v                  device bf16 [n][Hkv][d], not the cache itself
+ *   out_row_off           device int64 [B]: first output row of request b
+ *   out_row_cap           device int32 [B]: output rows request b owns
+ *   dev_status            SONIC_ERR_BAD_LAYOUT for a bad range, SONIC_ERR_CAPACITY for more rows
+ *                         than out_row_cap[b], SONIC_ERR_INVALID_ARG for more than max_rows;
+ *                         nothing is written for that request
+ */
+int32_t sonic_cache_expand_q4(int32_t batch, int32_t max_rows, int32_t num_kv_heads, int32_t head_dim,
+                              const void *k_cache, const void *k_scale, const void *v_cache, const void *v_scale,
+                              const int64_t *cache_row_off, const int32_t *cache_row_cap, const int32_t *row_begin,
+                              const int32_t *row_end, void *k, void *v, const int64_t *out_row_off,
+                              const int32_t *out_row_cap, int32_t *dev_status, void *stream);
+
+/* Bytes of device workspace sonic_compressed_decode_q4 needs, with a row_weight (weighted != 0) or without. */
+size_t sonic_decode_q4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t head_dim, int32_t max_ctx,
+                                       int32_t weighted);
+
+/*
+ * sonic_compressed_decode over 4-bit rows: k_new and v_new (bf16) are rounded and appended,
+ * and the attention reads every row, the appended one too, at its 4-bit values.
+ *   row_weight   NULL, or device fp32 [rows]: see sonic_compressed_decode_weighted
+ * The other arguments, outputs and errors are those of sonic_compressed_decode without
+ * row_role; a NaN row makes the outputs it reaches NaN.
+ */
+int32_t sonic_compressed_decode_q4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                   int32_t max_ctx, void *k_cache, void *k_scale, void *v_cache, void *v_scale,
+                                   const int64_t *cache_row_off, const int32_t *cache_row_cap, int32_t *cache_len,
+                                   const void *q, const void *k_new, const void *v_new, float softmax_scale, float *out,
+                                   float *row_weight, void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                   void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Row weights and eviction                                                  */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The prefill's key weights carried to the compacted rows:
+ *     row_weight[cache_row_off[b] + j] = key_weight[cu_seqlens[b] + keep_idx[cache_row_off[b] + j]]
+ * for j < cache_len[b], with keep_idx and cache_len as either compaction left them.
+ *   total_tokens  rows of key_weight (host value)
+ *   max_rows      host bound: cache_len[b] <= max_rows for every b
+ *   key_weight    device fp32 [T] (sonic_segment_attn_prefill);  row_weight: device fp32 [rows]
+ *   dev_status    SONIC_ERR_BAD_LAYOUT for inconsistent cu_seqlens, a negative length, or a
+ *                 keep_idx outside its request (the row keeps its weight),
+ *                 SONIC_ERR_INVALID_ARG for more rows than max_rows
+ */
+int32_t sonic_kv_compact_weights(int32_t batch, int32_t total_tokens, int32_t max_rows, const int32_t *cu_seqlens,
+                                 const float *key_weight, const int64_t *cache_row_off, const int32_t *cache_len,
+                                 const int32_t *keep_idx, float *row_weight, int32_t *dev_status, void *stream);
+
+/* Bytes of device workspace sonic_compressed_decode_weighted needs. */
+size_t sonic_decode_weighted_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t head_dim, int32_t max_ctx);
+
+/*
+ * sonic_compressed_decode over a compact bf16 cache that also keeps count of the attention
+ * each row receives: with p[h][r] the softmax weight of row r for q-head h,
+ *     row_weight[r] += (1 / Hq) * sum over h of p[h][r]      for rows r < cache_len[b],
+ * and the appended row's weight is set to that sum (what its place held before is
+ * dropped).  Requests that are not advanced keep their weights.  Reproducible: no atomic sums.
+ *   row_weight   device fp32 [rows], indexed like cache rows; sonic_kv_compact_weights, or
+ *                the caller, fills the rows a conversation starts with.  sonic_nexus_extend
+ *                does not know of it: after it the caller sets the rows it wrote.
+ * The other arguments, outputs and errors are those of sonic_compressed_decode without
+ * row_role; the workspace (sonic_decode_weighted_workspace_bytes) is larger by the scores,
+ * batch * num_q_heads * max_ctx floats.
+ */
+int32_t sonic_compressed_decode_weighted(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                         int32_t max_ctx, void *k_cache, void *v_cache, const int64_t *cache_row_off,
+                                         const int32_t *cache_row_cap, int32_t *cache_len, const void *q,
+                                         const void *k_new, const void *v_new, float softmax_scale, float *out,
+                                         float *row_weight, void *workspace, size_t workspace_bytes,
+                                         int32_t *dev_status, void *stream);
+
+/* Bytes of device workspace sonic_cache_evict needs (0 for negative sizes). */
+size_t sonic_cache_evict_workspace_bytes(int32_t batch, int32_t max_rows);
+
+/*
+ * Drop the rows of least weight of every request that has more than budget[b].  Of L rows
+ * the first H = min(keep_head[b], L) and the last T = min(keep_tail[b], L - H) stay, and of those
+ * between them the max(budget[b] - H - T, 0) of greatest row_weight (of equal weights the lower
+ * row; a NaN counts as -infinity).  A request of at most budget[b] rows keeps them all.  Kept rows
+ * keep their order and move, with their weights, to the front.
+ *
+ *   max_rows       host bound: cache_len[b] <= max_rows for every b
+ *   k_cache, v_cache   device bf16 [rows][Hkv][d] with k_scale = v_scale = NULL, or 4-bit
+ *                  rows with their scales
+ *   row_weight     device fp32 [rows]
+ *   keep_head, keep_tail, budget   device int32 [B], not negative
+ *   k_out ..       NULL: in place.  Request b's rows move down to cache_row_off[b] .., cache_len[b]
+ *                  becomes the kept count; rows behind those kept hold what they held.
+ *                  Otherwise another cache of the same kind, not overlapping the first (k_out,
+ *                  v_out, for 4-bit rows both scales, out_row_off int64 [B], out_row_cap int32
+ *                  [B], out_len int32 [B], out_weight fp32): request b's rows go to
+ *                  out_row_off[b] .., and the first cache is left as it is.
+ *   keep_idx       NULL, or device int32 [rows of the cache written]: each kept row's place
+ *                  (from 0) in its request before the call
+ *   workspace      device, 256-byte aligned, >= sonic_cache_evict_workspace_bytes(B, max_rows);
+ *                  contents need no initialisation
+ *   dev_status     SONIC_ERR_BAD_LAYOUT for a negative length, head, tail or budget, or a length
+ *                  above max_rows; SONIC_ERR_CAPACITY when more rows are kept than out_row_cap[b];
+ *                  then (as with any pending status) nothing is written for any request
+ * Returns SONIC_ERR_INVALID_ARG when only some of another cache's arrays are given.
+ */
+int32_t sonic_cache_evict(int32_t batch, int32_t max_rows, int32_t num_kv_heads, int32_t head_dim, void *k_cache,
+                          void *k_scale, void *v_cache, void *v_scale, const int64_t *cache_row_off,
+                          int32_t *cache_len, float *row_weight, const int32_t *keep_head, const int32_t *keep_tail,
+                          const int32_t *budget, void *k_out, void *k_scale_out, void *v_out, void *v_scale_out,
+                          const int64_t *out_row_off, const int32_t *out_row_cap, int32_t *out_len, float *out_weight,
+                          int32_t *keep_idx, void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                          void *stream);
 
 #ifdef __cplusplus
 }

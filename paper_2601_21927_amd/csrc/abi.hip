@@ -39,17 +39,30 @@ hipError_t launch_prefill(int D, int G, int grid, bool stats, int ks, int tile_r
                           hipStream_t stream);
 hipError_t launch_compact(int batch, int total_tokens, int max_seqlen, int Hkv, int D, const int32_t *cu,
                           const uint8_t *role,
-                          const uint16_t *k, const uint16_t *v, uint16_t *kc, uint16_t *vc, const int64_t *row_off,
+                          const uint16_t *k, const uint16_t *v, uint16_t *kc, uint16_t *vc, uint8_t *kscale,
+                          uint8_t *vscale, const int64_t *row_off,
                           const int32_t *row_cap, int32_t *cache_len, int32_t *keep_idx, int32_t *status,
                           hipStream_t stream);
 DecodeShape decode_shape(int batch, int Hkv, int G, int D, int max_ctx, bool masked, size_t part_bytes);
 size_t decode_ws_layout(int batch, int Hkv, size_t part_bytes, DecodeWs *ws, char *base);
 size_t decode_scratch_layout(int batch, int Hkv, size_t part_bytes, DecodeWs *ws, char *base);
 hipError_t decode_scratch(hipStream_t stream, char **base);
-hipError_t launch_decode(int batch, int Hq, int Hkv, int D, int max_ctx, const DecodeShape &sh, uint16_t *kc,
-                         uint16_t *vc, const int64_t *row_off, const int32_t *row_cap, int32_t *cache_len,
-                         const uint8_t *row_role, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
-                         float scale_log2, float *out, const DecodeWs &ws, int32_t *status, hipStream_t stream);
+hipError_t launch_decode(int batch, int Hq, int Hkv, int D, int max_ctx, const DecodeShape &sh, const DecodeCall &c,
+                         const DecodeWs &ws, hipStream_t stream);
+hipError_t launch_decode_weighted(int batch, int Hq, int Hkv, int D, int max_ctx, const DecodeShape &sh, const DecodeCall &c,
+                                  const DecodeRows &rows, const DecodeWs &ws, hipStream_t stream);
+hipError_t launch_decode_q4(int batch, int Hq, int Hkv, int D, int max_ctx, const DecodeShape &sh, const DecodeCall &c,
+                            const DecodeRows &rows, const DecodeWs &ws, hipStream_t stream);
+hipError_t launch_add_weights(int batch, int Hq, int max_ctx, const int64_t *row_off, const DecodeRows &rows, float *row_weight,
+                              hipStream_t stream);
+hipError_t launch_expand_q4(int batch, int max_rows, int Hkv, int D, const uint8_t *kc, const uint8_t *ks, const uint8_t *vc,
+                            const uint8_t *vs, const int64_t *row_off, const int32_t *row_cap, const int32_t *row_begin,
+                            const int32_t *row_end, uint16_t *k, uint16_t *v, const int64_t *out_off, const int32_t *out_cap,
+                            int32_t *status, hipStream_t stream);
+hipError_t launch_compact_weights(int batch, int total_tokens, int max_rows, const int32_t *cu, const float *key_weight,
+                                  const int64_t *row_off, const int32_t *cache_len, const int32_t *keep_idx, float *row_weight,
+                                  int32_t *status, hipStream_t stream);
+hipError_t launch_evict(const EvictCall &c, const EvictWs &ws, int Hkv, int D, hipStream_t stream);
 
 namespace {
 
@@ -532,24 +545,40 @@ int32_t sonic_nexus_recon_targets(int32_t batch, int32_t T, int32_t Dm, const in
 }
 
 // ---------------------------------------------------------------- compaction
-int32_t sonic_kv_compact(int32_t batch, int32_t total_tokens, int32_t max_seqlen, int32_t Hkv, int32_t d,
-                         const int32_t *cu_seqlens, const uint8_t *role, const void *k, const void *v, void *k_cache,
-                         void *v_cache, const int64_t *cache_row_off, const int32_t *cache_row_cap,
-                         int32_t *cache_len, int32_t *keep_idx, int32_t *dev_status, void *stream_) {
-  hipStream_t stream = static_cast<hipStream_t>(stream_);
+// Argument checks shared by the two compactions (see check_decode).
+static int32_t check_compact(int32_t batch, int32_t total_tokens, int32_t max_seqlen, int32_t Hkv, int32_t d,
+                             const int32_t *cu_seqlens, const uint8_t *role, const void *k, const void *v, const void *k_cache,
+                             const void *v_cache, const int64_t *cache_row_off, const int32_t *cache_row_cap,
+                             const int32_t *cache_len, const int32_t *keep_idx, const int32_t *dev_status, bool *empty) {
+  *empty = false;
   if (batch < 0 || total_tokens < 0 || max_seqlen < 0 || Hkv <= 0 || dev_status == nullptr)
     return SONIC_ERR_INVALID_ARG;
   if (batch > 65535) return SONIC_ERR_UNSUPPORTED;
   if (d != 64 && d != 128) return SONIC_ERR_UNSUPPORTED;
-  if (batch == 0) return SONIC_OK;
+  if (batch == 0) {
+    *empty = true;
+    return SONIC_OK;
+  }
   if (!cu_seqlens || !cache_row_off || !cache_row_cap || !cache_len) return SONIC_ERR_INVALID_ARG;
   if (total_tokens > 0 && (!role || !k || !v || !k_cache || !v_cache || !keep_idx)) return SONIC_ERR_INVALID_ARG;
   if (total_tokens > 0 && (!aligned(role, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(k_cache, 16) ||
                            !aligned(v_cache, 16)))
     return SONIC_ERR_INVALID_ARG;
+  return SONIC_OK;
+}
+
+int32_t sonic_kv_compact(int32_t batch, int32_t total_tokens, int32_t max_seqlen, int32_t Hkv, int32_t d,
+                         const int32_t *cu_seqlens, const uint8_t *role, const void *k, const void *v, void *k_cache,
+                         void *v_cache, const int64_t *cache_row_off, const int32_t *cache_row_cap,
+                         int32_t *cache_len, int32_t *keep_idx, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  bool empty = false;
+  const int32_t st = check_compact(batch, total_tokens, max_seqlen, Hkv, d, cu_seqlens, role, k, v, k_cache, v_cache, cache_row_off,
+                                   cache_row_cap, cache_len, keep_idx, dev_status, &empty);
+  if (st != SONIC_OK || empty) return st;
   hipError_t e = launch_compact(batch, total_tokens, max_seqlen, Hkv, d, cu_seqlens, role, static_cast<const uint16_t *>(k),
                                 static_cast<const uint16_t *>(v), static_cast<uint16_t *>(k_cache),
-                                static_cast<uint16_t *>(v_cache), cache_row_off, cache_row_cap, cache_len, keep_idx,
+                                static_cast<uint16_t *>(v_cache), nullptr, nullptr, cache_row_off, cache_row_cap, cache_len, keep_idx,
                                 dev_status, stream);
   return finish(e, dev_status, stream);
 }
@@ -598,6 +627,14 @@ static int32_t check_decode(int32_t batch, int32_t Hq, int32_t Hkv, int32_t d, i
   return SONIC_OK;
 }
 
+static DecodeCall decode_call(void *k_cache, void *v_cache, const int64_t *row_off, const int32_t *row_cap, int32_t *cache_len,
+                              const uint8_t *row_role, const void *q, const void *k_new, const void *v_new, float softmax_scale,
+                              float *out, int32_t *dev_status) {
+  return DecodeCall{static_cast<uint16_t *>(k_cache), static_cast<uint16_t *>(v_cache), row_off, row_cap, cache_len, row_role,
+                    static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new),
+                    static_cast<float>(softmax_scale * kLog2e), out, dev_status};
+}
+
 int32_t sonic_compressed_decode(int32_t batch, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_ctx, void *k_cache,
                                 void *v_cache, const int64_t *cache_row_off, const int32_t *cache_row_cap,
                                 int32_t *cache_len, const uint8_t *row_role, const void *q, const void *k_new,
@@ -615,11 +652,10 @@ int32_t sonic_compressed_decode(int32_t batch, int32_t Hq, int32_t Hkv, int32_t 
   if (workspace_bytes < counters || room < sh.part_bytes) return SONIC_ERR_WORKSPACE;
   DecodeWs ws;
   decode_ws_layout(batch, Hkv, sh.part_bytes, &ws, static_cast<char *>(workspace));
-  hipError_t e = launch_decode(batch, Hq, Hkv, d, max_ctx, sh, static_cast<uint16_t *>(k_cache),
-                               static_cast<uint16_t *>(v_cache), cache_row_off, cache_row_cap, cache_len, row_role,
-                               static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_new),
-                               static_cast<const uint16_t *>(v_new), static_cast<float>(softmax_scale * kLog2e), out,
-                               ws, dev_status, stream);
+  hipError_t e = launch_decode(batch, Hq, Hkv, d, max_ctx, sh,
+                               decode_call(k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, row_role, q, k_new, v_new,
+                                           softmax_scale, out, dev_status),
+                               ws, stream);
   return finish(e, dev_status, stream);
 }
 
@@ -642,12 +678,206 @@ int32_t sonic_compressed_decode_noalloc(int32_t batch, int32_t Hq, int32_t Hkv, 
   if (e != hipSuccess) return SONIC_ERR_HIP;
   DecodeWs ws;
   decode_scratch_layout(batch, Hkv, sh.part_bytes, &ws, base);
-  e = launch_decode(batch, Hq, Hkv, d, max_ctx, sh, static_cast<uint16_t *>(k_cache),
-                    static_cast<uint16_t *>(v_cache), cache_row_off, cache_row_cap, cache_len, row_role,
-                    static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_new),
-                    static_cast<const uint16_t *>(v_new), static_cast<float>(softmax_scale * kLog2e), out, ws,
-                    dev_status, stream);
+  e = launch_decode(batch, Hq, Hkv, d, max_ctx, sh,
+                    decode_call(k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, row_role, q, k_new, v_new,
+                                softmax_scale, out, dev_status),
+                    ws, stream);
   return finish(e, dev_status, stream);
+}
+
+// ---------------------------------------------------------------- decode with row weights, 4-bit rows
+// Behind the decode workspace: the advanced requests, the normalisers and the scores.
+static size_t weighted_ws_layout(int32_t batch, int32_t Hq, int32_t max_ctx, char *base, DecodeRows *rows) {
+  const size_t stride = align_up(max_ctx, 16);
+  const size_t f_bytes = align_up(static_cast<size_t>(batch) * sizeof(int32_t), 256);
+  const size_t l_bytes = align_up(static_cast<size_t>(batch) * Hq * sizeof(float), 256);
+  if (base) {
+    rows->fresh = reinterpret_cast<int32_t *>(base);
+    rows->lse = reinterpret_cast<float *>(base + f_bytes);
+    rows->scores = reinterpret_cast<float *>(base + f_bytes + l_bytes);
+    rows->stride = stride;
+  }
+  return f_bytes + l_bytes + static_cast<size_t>(batch) * Hq * stride * sizeof(float);
+}
+
+size_t sonic_decode_weighted_workspace_bytes(int32_t batch, int32_t Hq, int32_t d, int32_t max_ctx) {
+  if (batch <= 0 || Hq <= 0 || max_ctx <= 0) return 256;
+  return align_up(sonic_decode_workspace_bytes(batch, Hq, d, max_ctx) + weighted_ws_layout(batch, Hq, max_ctx, nullptr, nullptr), 256);
+}
+
+size_t sonic_decode_q4_workspace_bytes(int32_t batch, int32_t Hq, int32_t d, int32_t max_ctx, int32_t weighted) {
+  return weighted ? sonic_decode_weighted_workspace_bytes(batch, Hq, d, max_ctx) : sonic_decode_workspace_bytes(batch, Hq, d, max_ctx);
+}
+
+int32_t sonic_compressed_decode_weighted(int32_t batch, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_ctx, void *k_cache,
+                                         void *v_cache, const int64_t *cache_row_off, const int32_t *cache_row_cap,
+                                         int32_t *cache_len, const void *q, const void *k_new, const void *v_new,
+                                         float softmax_scale, float *out, float *row_weight, void *workspace,
+                                         size_t workspace_bytes, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  bool empty = false;
+  const int32_t st = check_decode(batch, Hq, Hkv, d, max_ctx, k_cache, v_cache, cache_row_off, cache_row_cap,
+                                  cache_len, q, k_new, v_new, &softmax_scale, out, dev_status, &empty);
+  if (st != SONIC_OK || empty) return st;
+  if (!row_weight || !aligned(row_weight, 4) || !workspace || !aligned(workspace, 256)) return SONIC_ERR_INVALID_ARG;
+  if (workspace_bytes < sonic_decode_weighted_workspace_bytes(batch, Hq, d, max_ctx)) return SONIC_ERR_WORKSPACE;
+  const DecodeShape sh = decode_shape(batch, Hkv, Hq / Hkv, d, max_ctx, false, SIZE_MAX);
+  char *base = static_cast<char *>(workspace);
+  DecodeWs ws;
+  decode_ws_layout(batch, Hkv, sh.part_bytes, &ws, base);
+  DecodeRows rows{};
+  weighted_ws_layout(batch, Hq, max_ctx, base + sonic_decode_workspace_bytes(batch, Hq, d, max_ctx), &rows);
+  hipError_t e = launch_decode_weighted(batch, Hq, Hkv, d, max_ctx, sh,
+                                        decode_call(k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, nullptr, q, k_new,
+                                                    v_new, softmax_scale, out, dev_status),
+                                        rows, ws, stream);
+  if (e == hipSuccess) e = launch_add_weights(batch, Hq, max_ctx, cache_row_off, rows, row_weight, stream);
+  return finish(e, dev_status, stream);
+}
+
+int32_t sonic_compressed_decode_q4(int32_t batch, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_ctx, void *k_cache,
+                                   void *k_scale, void *v_cache, void *v_scale, const int64_t *cache_row_off,
+                                   const int32_t *cache_row_cap, int32_t *cache_len, const void *q, const void *k_new,
+                                   const void *v_new, float softmax_scale, float *out, float *row_weight, void *workspace,
+                                   size_t workspace_bytes, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  bool empty = false;
+  const int32_t st = check_decode(batch, Hq, Hkv, d, max_ctx, k_cache, v_cache, cache_row_off, cache_row_cap,
+                                  cache_len, q, k_new, v_new, &softmax_scale, out, dev_status, &empty);
+  if (st != SONIC_OK || empty) return st;
+  if (!k_scale || !v_scale || !aligned(k_scale, 4) || !aligned(v_scale, 4) || !aligned(row_weight, 4) || !workspace ||
+      !aligned(workspace, 256))
+    return SONIC_ERR_INVALID_ARG;
+  if (workspace_bytes < sonic_decode_q4_workspace_bytes(batch, Hq, d, max_ctx, row_weight != nullptr)) return SONIC_ERR_WORKSPACE;
+  const DecodeShape sh = decode_shape(batch, Hkv, Hq / Hkv, d, max_ctx, false, SIZE_MAX);
+  char *base = static_cast<char *>(workspace);
+  DecodeWs ws;
+  decode_ws_layout(batch, Hkv, sh.part_bytes, &ws, base);
+  DecodeRows rows{};
+  if (row_weight != nullptr)
+    weighted_ws_layout(batch, Hq, max_ctx, base + sonic_decode_q4_workspace_bytes(batch, Hq, d, max_ctx, 0), &rows);
+  rows.ks = static_cast<uint8_t *>(k_scale);
+  rows.vs = static_cast<uint8_t *>(v_scale);
+  hipError_t e = launch_decode_q4(batch, Hq, Hkv, d, max_ctx, sh,
+                                  decode_call(k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, nullptr, q, k_new, v_new,
+                                              softmax_scale, out, dev_status),
+                                  rows, ws, stream);
+  if (e == hipSuccess && row_weight != nullptr) e = launch_add_weights(batch, Hq, max_ctx, cache_row_off, rows, row_weight, stream);
+  return finish(e, dev_status, stream);
+}
+
+// ---------------------------------------------------------------- 4-bit rows written and read back
+int32_t sonic_kv_compact_q4(int32_t batch, int32_t total_tokens, int32_t max_seqlen, int32_t Hkv, int32_t d,
+                            const int32_t *cu_seqlens, const uint8_t *role, const void *k, const void *v, void *k_cache,
+                            void *k_scale, void *v_cache, void *v_scale, const int64_t *cache_row_off,
+                            const int32_t *cache_row_cap, int32_t *cache_len, int32_t *keep_idx, int32_t *dev_status,
+                            void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  bool empty = false;
+  const int32_t st = check_compact(batch, total_tokens, max_seqlen, Hkv, d, cu_seqlens, role, k, v, k_cache, v_cache, cache_row_off,
+                                   cache_row_cap, cache_len, keep_idx, dev_status, &empty);
+  if (st != SONIC_OK || empty) return st;
+  if (!k_scale || !v_scale || !aligned(k_scale, 4) || !aligned(v_scale, 4)) return SONIC_ERR_INVALID_ARG;
+  const hipError_t e = launch_compact(batch, total_tokens, max_seqlen, Hkv, d, cu_seqlens, role, static_cast<const uint16_t *>(k),
+                                      static_cast<const uint16_t *>(v), static_cast<uint16_t *>(k_cache),
+                                      static_cast<uint16_t *>(v_cache), static_cast<uint8_t *>(k_scale),
+                                      static_cast<uint8_t *>(v_scale), cache_row_off, cache_row_cap, cache_len, keep_idx, dev_status,
+                                      stream);
+  return finish(e, dev_status, stream);
+}
+
+int32_t sonic_cache_expand_q4(int32_t batch, int32_t max_rows, int32_t Hkv, int32_t d, const void *k_cache, const void *k_scale,
+                              const void *v_cache, const void *v_scale, const int64_t *cache_row_off, const int32_t *cache_row_cap,
+                              const int32_t *row_begin, const int32_t *row_end, void *k, void *v, const int64_t *out_row_off,
+                              const int32_t *out_row_cap, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (batch < 0 || max_rows < 0 || Hkv <= 0 || dev_status == nullptr) return SONIC_ERR_INVALID_ARG;
+  if (batch > 65535) return SONIC_ERR_UNSUPPORTED;
+  if (d != 64 && d != 128) return SONIC_ERR_UNSUPPORTED;
+  if (batch == 0) return SONIC_OK;
+  if (!k_cache || !k_scale || !v_cache || !v_scale || !cache_row_off || !cache_row_cap || !row_begin || !row_end || !k || !v ||
+      !out_row_off || !out_row_cap)
+    return SONIC_ERR_INVALID_ARG;
+  if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4) || !aligned(k, 16) ||
+      !aligned(v, 16))
+    return SONIC_ERR_INVALID_ARG;
+  const hipError_t e = launch_expand_q4(batch, max_rows, Hkv, d, static_cast<const uint8_t *>(k_cache),
+                                        static_cast<const uint8_t *>(k_scale), static_cast<const uint8_t *>(v_cache),
+                                        static_cast<const uint8_t *>(v_scale), cache_row_off, cache_row_cap, row_begin, row_end,
+                                        static_cast<uint16_t *>(k), static_cast<uint16_t *>(v), out_row_off, out_row_cap,
+                                        dev_status, stream);
+  return finish(e, dev_status, stream);
+}
+
+// ---------------------------------------------------------------- eviction
+int32_t sonic_kv_compact_weights(int32_t batch, int32_t total_tokens, int32_t max_rows, const int32_t *cu_seqlens,
+                                 const float *key_weight, const int64_t *cache_row_off, const int32_t *cache_len,
+                                 const int32_t *keep_idx, float *row_weight, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (batch < 0 || total_tokens < 0 || max_rows < 0 || dev_status == nullptr) return SONIC_ERR_INVALID_ARG;
+  if (batch > 65535) return SONIC_ERR_UNSUPPORTED;
+  if (batch == 0) return SONIC_OK;
+  if (!cu_seqlens || !cache_row_off || !cache_len) return SONIC_ERR_INVALID_ARG;
+  if (max_rows > 0 && (!key_weight || !keep_idx || !row_weight)) return SONIC_ERR_INVALID_ARG;
+  if (!aligned(key_weight, 4) || !aligned(row_weight, 4)) return SONIC_ERR_INVALID_ARG;
+  const hipError_t e = launch_compact_weights(batch, total_tokens, max_rows, cu_seqlens, key_weight, cache_row_off, cache_len,
+                                              keep_idx, row_weight, dev_status, stream);
+  return finish(e, dev_status, stream);
+}
+
+static size_t evict_ws_layout(int32_t batch, int32_t max_rows, char *base, EvictWs *ws) {
+  const size_t r_bytes = align_up(static_cast<size_t>(batch) * sizeof(int2), 256);
+  if (base) {
+    ws->ctrl = reinterpret_cast<int32_t *>(base);
+    ws->req = reinterpret_cast<int2 *>(base + 256);
+    ws->list = reinterpret_cast<int32_t *>(base + 256 + r_bytes);
+  }
+  return align_up(256 + r_bytes + static_cast<size_t>(batch) * max_rows * sizeof(int32_t), 256);
+}
+
+size_t sonic_cache_evict_workspace_bytes(int32_t batch, int32_t max_rows) {
+  if (batch < 0 || max_rows < 0) return 0;
+  return evict_ws_layout(batch, max_rows, nullptr, nullptr);
+}
+
+int32_t sonic_cache_evict(int32_t batch, int32_t max_rows, int32_t Hkv, int32_t d, void *k_cache, void *k_scale, void *v_cache,
+                          void *v_scale, const int64_t *cache_row_off, int32_t *cache_len, float *row_weight,
+                          const int32_t *keep_head, const int32_t *keep_tail, const int32_t *budget, void *k_out,
+                          void *k_scale_out, void *v_out, void *v_scale_out, const int64_t *out_row_off,
+                          const int32_t *out_row_cap, int32_t *out_len, float *out_weight, int32_t *keep_idx, void *workspace,
+                          size_t workspace_bytes, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (batch < 0 || max_rows < 0 || Hkv <= 0 || dev_status == nullptr) return SONIC_ERR_INVALID_ARG;
+  if (batch > 65535) return SONIC_ERR_UNSUPPORTED;
+  if (d != 64 && d != 128) return SONIC_ERR_UNSUPPORTED;
+  if (batch == 0) return SONIC_OK;
+  if (!k_cache || !v_cache || !cache_row_off || !cache_len || !row_weight || !keep_head || !keep_tail || !budget || !workspace)
+    return SONIC_ERR_INVALID_ARG;
+  const bool q4 = k_scale != nullptr, away = k_out != nullptr;
+  if ((v_scale != nullptr) != q4) return SONIC_ERR_INVALID_ARG;
+  // to another cache: all of its arrays, none of them the source's; in place: none
+  const void *out[] = {v_out, out_row_off, out_row_cap, out_len, out_weight};
+  for (const void *p : out)
+    if ((p != nullptr) != away) return SONIC_ERR_INVALID_ARG;
+  if ((k_scale_out != nullptr) != (q4 && away) || (v_scale_out != nullptr) != (q4 && away)) return SONIC_ERR_INVALID_ARG;
+  if (away && (k_out == k_cache || v_out == v_cache || out_weight == row_weight || out_len == cache_len ||
+               (q4 && (k_scale_out == k_scale || v_scale_out == v_scale))))
+    return SONIC_ERR_INVALID_ARG;
+  for (const void *p : {static_cast<const void *>(k_cache), static_cast<const void *>(v_cache), static_cast<const void *>(k_out),
+                        static_cast<const void *>(v_out)})
+    if (!aligned(p, 16)) return SONIC_ERR_INVALID_ARG;
+  for (const void *p : {static_cast<const void *>(k_scale), static_cast<const void *>(v_scale), static_cast<const void *>(k_scale_out),
+                        static_cast<const void *>(v_scale_out), static_cast<const void *>(row_weight),
+                        static_cast<const void *>(out_weight)})
+    if (!aligned(p, 4)) return SONIC_ERR_INVALID_ARG;
+  if (!aligned(workspace, 256)) return SONIC_ERR_INVALID_ARG;
+  EvictWs ws;
+  if (workspace_bytes < evict_ws_layout(batch, max_rows, static_cast<char *>(workspace), &ws)) return SONIC_ERR_WORKSPACE;
+  const EvictCall c{batch, max_rows, k_cache, v_cache, static_cast<const uint8_t *>(k_scale), static_cast<const uint8_t *>(v_scale),
+                    cache_row_off, cache_len, row_weight, keep_head, keep_tail, budget, k_out, v_out,
+                    static_cast<uint8_t *>(k_scale_out), static_cast<uint8_t *>(v_scale_out), out_row_off, out_row_cap, out_len,
+                    out_weight, keep_idx, dev_status};
+  return finish(launch_evict(c, ws, Hkv, d, stream), dev_status, stream);
 }
 
 }  // extern "C"

@@ -213,6 +213,55 @@ struct DecodeWs {
   float *part;        // partials: acc[G][D] of every split, then (max, sum)[G] of every split
 };
 
+// What the 4-bit and the weighted decode add.  rows.hip turns scores and normalisers into row weights.
+struct DecodeRows {
+  uint8_t *ks;        // 4-bit rows: scale bytes of K and V, [rows][Hkv][D / 32]
+  uint8_t *vs;
+  float *scores;      // [B][Hq][stride] log2-domain scores of every context row
+  float *lse;         // [B][Hq] log2-domain softmax normaliser
+  int32_t *fresh;     // [B] context rows of the requests that this call advanced, 0 for the others
+  size_t stride;      // rows a request's scores have room for, a multiple of 16
+};
+
+// The tensors of a decode call (k and v as codes for 4-bit rows).
+struct DecodeCall {
+  uint16_t *kc, *vc;
+  const int64_t *row_off;
+  const int32_t *row_cap;
+  int32_t *cache_len;
+  const uint8_t *row_role;
+  const uint16_t *q, *k_new, *v_new;
+  float scale_log2;
+  float *out;
+  int32_t *status;
+};
+
+// The tensors of an eviction; k_out is null in place.
+struct EvictCall {
+  int batch, max_rows;
+  const void *k, *v;              // bf16 rows, or codes
+  const uint8_t *ks, *vs;         // null for bf16 rows
+  const int64_t *row_off;
+  int32_t *cache_len;             // written in place
+  float *row_weight;              // written in place
+  const int32_t *keep_head, *keep_tail, *budget;
+  void *k_out, *v_out;
+  uint8_t *ks_out, *vs_out;
+  const int64_t *out_row_off;
+  const int32_t *out_row_cap;
+  int32_t *out_len;
+  float *out_weight;
+  int32_t *keep_idx;              // null, or the kept rows' old places
+  int32_t *status;
+};
+
+// Workspace of an eviction.
+struct EvictWs {
+  int32_t *ctrl;     // [0]: the call is to be done
+  int2 *req;         // [B] rows kept, rows before the first dropped one
+  int32_t *list;     // [B][max_rows] the kept rows in order
+};
+
 // How a decode call is cut into workgroups.
 struct DecodeShape {
   int splits;         // workgroups per (request, kv-head); shared rows: per kv-head

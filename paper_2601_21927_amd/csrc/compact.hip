@@ -17,7 +17,12 @@
 // Destination row = cache_row_off[b] + (kept before) + rank.  Rows past the
 // request's capacity are not written; SONIC_ERR_CAPACITY is raised instead.
 // role is read only inside its total_tokens bytes.
+//
+// Q4: the rows go to a 4-bit cache (q4.h).  A thread's unit is the same eight values;
+// four neighbouring lanes hold a block of 32, find its scale with two lane exchanges
+// and store four bytes of codes each, the first of them the scale byte.
 #include "common.h"
+#include "q4.h"
 #include "scan.h"
 
 namespace sonic {
@@ -40,11 +45,22 @@ __device__ __forceinline__ int kept_in_dword(uint32_t w, int lo, int hi) {
   return 4 - __popc(zero_hi);
 }
 
-template <int D>
+// Unit `at` (eight values) of a 4-bit tensor; its block's other three are the neighbouring lanes'.
+__device__ __forceinline__ void store_q4(const u32x4 &x, size_t at, uint32_t *codes, uint8_t *scale) {
+  const uint32_t w[4] = {x[0], x[1], x[2], x[3]};
+  int top = static_cast<int>(q4_top(w));
+  top = max(top, __builtin_amdgcn_update_dpp(0, top, 0xB1, 0xF, 0xF, false));   // quad_perm: lane ^ 1
+  top = max(top, __builtin_amdgcn_update_dpp(0, top, 0x4E, 0xF, 0xF, false));   // quad_perm: lane ^ 2
+  const uint32_t byte = q4_scale_byte(top);
+  codes[at] = q4_encode8(w[0], w[1], w[2], w[3], byte);
+  if (at % 4 == 0) scale[at / 4] = static_cast<uint8_t>(byte);
+}
+
+template <int D, bool Q4>
 __global__ __launch_bounds__(kCompactThreads) void compact_kernel(
     const int32_t *__restrict__ cu, const uint8_t *__restrict__ role, const uint16_t *__restrict__ k,
-    const uint16_t *__restrict__ v, uint16_t *__restrict__ kc, uint16_t *__restrict__ vc,
-    const int64_t *__restrict__ row_off, const int32_t *__restrict__ row_cap, int32_t *__restrict__ cache_len,
+    const uint16_t *__restrict__ v, uint16_t *__restrict__ kc, uint16_t *__restrict__ vc, uint8_t *__restrict__ kscale,
+    uint8_t *__restrict__ vscale, const int64_t *__restrict__ row_off, const int32_t *__restrict__ row_cap, int32_t *__restrict__ cache_len,
     int32_t *__restrict__ keep_idx, int32_t *status, int total_tokens, int Hkv) {
   __shared__ int lds[2 * (kCompactThreads / kWave)];
   __shared__ int16_t kept_pos[kCompactChunk];
@@ -171,30 +187,38 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(
 #pragma unroll
     for (int i = 0; i < kCopyUnroll; ++i) {
       if (u0 + i * kCompactThreads < nunits) {
-        kd[dst[i]] = ku[i];
-        vd[dst[i]] = vu[i];
+        if constexpr (Q4) {
+          store_q4(ku[i], dst[i], reinterpret_cast<uint32_t *>(kc), kscale);
+          store_q4(vu[i], dst[i], reinterpret_cast<uint32_t *>(vc), vscale);
+        } else {
+          kd[dst[i]] = ku[i];
+          vd[dst[i]] = vu[i];
+        }
       }
     }
   }
 }
 
+// kscale == nullptr: bf16 rows
 hipError_t launch_compact(int batch, int total_tokens, int max_seqlen, int Hkv, int D, const int32_t *cu,
                           const uint8_t *role,
-                          const uint16_t *k, const uint16_t *v, uint16_t *kc, uint16_t *vc, const int64_t *row_off,
+                          const uint16_t *k, const uint16_t *v, uint16_t *kc, uint16_t *vc, uint8_t *kscale,
+                          uint8_t *vscale, const int64_t *row_off,
                           const int32_t *row_cap, int32_t *cache_len, int32_t *keep_idx, int32_t *status,
                           hipStream_t stream) {
   const int chunks = max(1, (max_seqlen + kCompactChunk - 1) / kCompactChunk);
   const long cb = static_cast<long>(chunks) * batch;
   const int slices = static_cast<int>(max(1L, min(static_cast<long>(kCompactMaxSlices), (2048 + cb - 1) / cb)));
   dim3 grid(chunks, batch, slices);
-  if (D == 64)
-    compact_kernel<64><<<grid, dim3(kCompactThreads), 0, stream>>>(cu, role, k, v, kc, vc, row_off, row_cap,
-                                                                   cache_len, keep_idx, status, total_tokens, Hkv);
-  else if (D == 128)
-    compact_kernel<128><<<grid, dim3(kCompactThreads), 0, stream>>>(cu, role, k, v, kc, vc, row_off, row_cap,
-                                                                    cache_len, keep_idx, status, total_tokens, Hkv);
-  else
-    return hipErrorInvalidValue;
+#define GO(DD, Q4)                                                                                              \
+  compact_kernel<DD, Q4><<<grid, dim3(kCompactThreads), 0, stream>>>(cu, role, k, v, kc, vc, kscale, vscale, row_off, \
+                                                                     row_cap, cache_len, keep_idx, status, total_tokens, Hkv)
+  if (D == 64 && kscale == nullptr) GO(64, false);
+  else if (D == 128 && kscale == nullptr) GO(128, false);
+  else if (D == 64) GO(64, true);
+  else if (D == 128) GO(128, true);
+  else return hipErrorInvalidValue;
+#undef GO
   return hipGetLastError();
 }
 

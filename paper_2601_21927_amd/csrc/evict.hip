@@ -1,0 +1,284 @@
+// Eviction by accumulated attention weight: of a request's rows the first and the last ones stay, and of those
+// between them the heaviest, up to a budget.  What stays keeps its order, because the rows' order is what the
+// next-turn step reads (system prompt, Nexus rows, the turn's rows).
+//
+// select_kernel, one workgroup per request: checks the lengths of every request, so that a call is done for all or
+// for none, finds the weight that separates kept from dropped rows by a radix search over the weights' order (four
+// passes of eight bits, histograms in LDS; a few bytes per row, served from L2), and lists the kept rows.  It writes
+// to the workspace only.
+// move_kernel, to another cache: every kept row is read and written once, in parallel over rows.
+// move_in_place_kernel: row j goes down to j from list[j] >= j, so a workgroup that walks the rows upwards, loading a
+// batch before it stores it, never overwrites a row it has yet to read; workgroups split the rows' bytes into
+// columns.  Rows before the first dropped one are not touched.
+#include <algorithm>
+
+#include "common.h"
+#include "scan.h"
+
+namespace sonic {
+
+constexpr int kSelectThreads = 1024;
+constexpr int kSelectRows = 4;                              // consecutive rows of a thread
+constexpr int kSelectChunk = kSelectThreads * kSelectRows;
+constexpr int kMoveThreads = 256;
+constexpr int kMoveUnroll = 4;
+
+// A request's rows, cut into head, middle and tail.
+struct EvictReq {
+  int len, head, tail, kept;
+};
+__device__ __forceinline__ int evict_check(int j, const EvictCall &c, EvictReq *r) {
+  const int len = c.cache_len[j], head = c.keep_head[j], tail = c.keep_tail[j], budget = c.budget[j];
+  *r = EvictReq{0, 0, 0, 0};
+  if (len < 0 || len > c.max_rows || head < 0 || tail < 0 || budget < 0) return SONIC_ERR_BAD_LAYOUT;
+  r->len = len;
+  r->head = min(head, len);
+  r->tail = min(tail, len - r->head);
+  r->kept = len <= budget ? len : max(r->head + r->tail, budget);
+  if (c.out_row_cap != nullptr && r->kept > c.out_row_cap[j]) return SONIC_ERR_CAPACITY;
+  return 0;
+}
+
+// Weights as unsigned integers of the same order; NaN as -infinity, -0 as 0.
+__device__ __forceinline__ uint32_t weight_key(float w) {
+  const uint32_t u = __float_as_uint(w == w ? w + 0.f : -INFINITY);
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, EvictWs ws) {
+  __shared__ int lds[2 * (kSelectThreads / kWave)];
+  __shared__ int hist[256];
+  __shared__ int s_ok, s_digit, s_rest, s_first;
+  const int b = blockIdx.x;
+  // workgroup 0's look at the status word decides for the whole call
+  const bool clear = b != 0 || block_status_clear(c.status, &s_ok);
+  EvictReq own;
+  const int own_code = evict_check(b, c, &own);
+  int bad = 0;
+  for (int j = threadIdx.x; j < c.batch; j += kSelectThreads) {
+    EvictReq r;
+    bad |= evict_check(j, c, &r) != 0;
+  }
+  bad = __syncthreads_or(bad);
+  if (own_code != 0 && threadIdx.x == 0) raise_status(c.status, own_code);
+  if (b == 0 && threadIdx.x == 0) ws.ctrl[0] = clear && !bad;
+  if (bad || !clear) return;
+
+  const float *w = c.row_weight + c.row_off[b];
+  int32_t *list = ws.list + static_cast<size_t>(b) * c.max_rows;
+  const int lo = own.head, hi = own.len - own.tail;
+  int take = own.kept - own.head - own.tail;   // of the middle rows
+  // the key of the lightest kept row (threshold), and how many of the rows at it are kept (rest)
+  uint32_t threshold = 0;
+  int rest = 0;
+  if (take == hi - lo) {
+    threshold = 0, rest = 0;   // all: every key is above 0 (only negative NaN patterns map to 0, and those are -infinity)
+  } else if (take == 0) {
+    threshold = 0xFFFFFFFFu;
+  } else {
+    int need = take;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      for (int i = threadIdx.x; i < 256; i += kSelectThreads) hist[i] = 0;
+      __syncthreads();
+      for (int r = lo + threadIdx.x; r < hi; r += kSelectThreads) {
+        const uint32_t key = weight_key(w[r]);
+        if (shift == 24 || (key >> (shift + 8)) == (threshold >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255], 1);
+      }
+      __syncthreads();
+      if (threadIdx.x < kWave) {
+        // lane l holds digits 255 - 4 l down to 252 - 4 l: the digit where the count from above reaches `need`
+        int h[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += h[i] = hist[255 - 4 * threadIdx.x - i];
+        int above = wave_scan(sum) - sum;
+        if (above < need && above + sum >= need) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (above < need && above + h[i] >= need) {
+              s_digit = 255 - 4 * threadIdx.x - i;
+              s_rest = need - above;
+            }
+            above += h[i];
+          }
+        }
+      }
+      __syncthreads();
+      threshold |= static_cast<uint32_t>(s_digit) << shift;
+      need = s_rest;
+    }
+    rest = need;
+  }
+
+  // the list, in row order
+  if (threadIdx.x == 0) s_first = own.kept;
+  __syncthreads();
+  int listed = 0, equal = 0;
+  for (int base = 0; base < own.len; base += kSelectChunk) {
+    const int r0 = base + kSelectRows * threadIdx.x;
+    uint32_t key[kSelectRows];
+    int sure = 0, ties = 0;
+#pragma unroll
+    for (int i = 0; i < kSelectRows; ++i) {
+      const int r = r0 + i;
+      // past the end: as if dropped; head and tail: as if heavier than any
+      key[i] = r >= own.len ? 0u : r < lo || r >= hi ? 0xFFFFFFFFu : weight_key(w[r]);
+      sure += r < own.len && (r < lo || r >= hi || key[i] > threshold);
+      ties += r >= lo && r < hi && key[i] == threshold;
+    }
+    // a tie is kept while fewer than `rest` come before it
+    const int x[2] = {sure, ties};
+    int below[2], total[2];
+    block_int_scan_n<kSelectThreads, 2>(x, below, total, lds);
+    int tie_rank = equal + below[1];
+    int at = listed + below[0] + min(tie_rank, rest) - min(equal, rest);
+#pragma unroll
+    for (int i = 0; i < kSelectRows; ++i) {
+      const int r = r0 + i;
+      if (r >= own.len) break;
+      const bool mid = r >= lo && r < hi;
+      const bool tie = mid && key[i] == threshold;
+      if (!mid || key[i] > threshold || (tie && tie_rank < rest)) list[at++] = r;
+      else if (at == r) s_first = r;   // the first dropped row: those before it stay where they are
+      tie_rank += tie;
+    }
+    listed += total[0] + min(equal + total[1], rest) - min(equal, rest);
+    equal += total[1];
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) ws.req[b] = make_int2(own.kept, s_first);
+}
+
+// To another cache.  Grid (chunks of 16-byte units of the kept rows, requests).
+template <typename SCALE>
+__global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictCall c, EvictWs ws, int row_units, int scale_units) {
+  if (ws.ctrl[0] == 0) return;
+  const int b = blockIdx.y;
+  const int kept = ws.req[b].x;
+  const int32_t *list = ws.list + static_cast<size_t>(b) * c.max_rows;
+  const size_t src0 = c.row_off[b], dst0 = c.out_row_off[b];
+  const long first = static_cast<long>(blockIdx.x) * kMoveThreads + threadIdx.x, step = static_cast<long>(gridDim.x) * kMoveThreads;
+  for (long j = first; j < kept; j += step) {
+    const int r = list[j];
+    c.out_weight[dst0 + j] = c.row_weight[src0 + r];
+    if (c.keep_idx != nullptr) c.keep_idx[dst0 + j] = r;
+  }
+  const u32x4 *k = reinterpret_cast<const u32x4 *>(c.k), *v = reinterpret_cast<const u32x4 *>(c.v);
+  u32x4 *ko = reinterpret_cast<u32x4 *>(c.k_out), *vo = reinterpret_cast<u32x4 *>(c.v_out);
+  const long total = static_cast<long>(kept) * row_units;
+  for (long u0 = first; u0 < total; u0 += step * kMoveUnroll) {
+    u32x4 x[kMoveUnroll], y[kMoveUnroll];
+#pragma unroll
+    for (int i = 0; i < kMoveUnroll; ++i) {
+      const long u = u0 + i * step;
+      if (u < total) {
+        const long j = u / row_units;
+        const size_t src = (src0 + list[j]) * row_units + (u - j * row_units);
+        x[i] = k[src];
+        y[i] = v[src];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kMoveUnroll; ++i) {
+      const long u = u0 + i * step;
+      if (u < total) {
+        ko[dst0 * row_units + u] = x[i];
+        vo[dst0 * row_units + u] = y[i];
+      }
+    }
+  }
+  if (scale_units > 0) {
+    const SCALE *ks = reinterpret_cast<const SCALE *>(c.ks), *vs = reinterpret_cast<const SCALE *>(c.vs);
+    SCALE *kso = reinterpret_cast<SCALE *>(c.ks_out), *vso = reinterpret_cast<SCALE *>(c.vs_out);
+    const long n = static_cast<long>(kept) * scale_units;
+    for (long u = first; u < n; u += step) {
+      const long j = u / scale_units;
+      const size_t src = (src0 + list[j]) * scale_units + (u - j * scale_units);
+      kso[dst0 * scale_units + u] = ks[src];
+      vso[dst0 * scale_units + u] = vs[src];
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) c.out_len[b] = kept;
+}
+
+// Rows first .. kept of one column (units [unit0, unit0 + units) of each row of `plane`), downwards in place.
+template <typename UNIT>
+__device__ __forceinline__ void walk_down(UNIT *plane, size_t row0, int row_units, int unit0, int units, const int32_t *list,
+                                          int first, int kept) {
+  const int rows = kMoveThreads / units;   // rows that the threads cover at once
+  const int i = threadIdx.x / units, u = threadIdx.x % units;
+  const bool active = i < rows;
+  UNIT *p = plane + row0 * row_units + unit0 + u;
+  for (int j0 = first; j0 < kept; j0 += rows * kMoveUnroll) {
+    UNIT x[kMoveUnroll];
+#pragma unroll
+    for (int n = 0; n < kMoveUnroll; ++n) {
+      const int j = j0 + n * rows + i;
+      if (active && j < kept) x[n] = p[static_cast<size_t>(list[j]) * row_units];
+    }
+    __syncthreads();   // the batch is loaded by every thread: rows below j0 + rows * kMoveUnroll may be overwritten
+#pragma unroll
+    for (int n = 0; n < kMoveUnroll; ++n) {
+      const int j = j0 + n * rows + i;
+      if (active && j < kept) p[static_cast<size_t>(j) * row_units] = x[n];
+    }
+  }
+}
+
+// In place.  Grid (columns, requests): the columns of K, of V, of the scales of K and V, and the weights.
+template <typename SCALE>
+__global__ __launch_bounds__(kMoveThreads) void move_in_place_kernel(EvictCall c, EvictWs ws, int row_units, int col_units,
+                                                                     int scale_units) {
+  if (ws.ctrl[0] == 0) return;
+  const int b = blockIdx.y;
+  const int kept = ws.req[b].x, first = ws.req[b].y;
+  const int32_t *list = ws.list + static_cast<size_t>(b) * c.max_rows;
+  const size_t row0 = c.row_off[b];
+  const int cols = (row_units + col_units - 1) / col_units;
+  int col = blockIdx.x;
+  if (col < 2 * cols) {
+    u32x4 *plane = reinterpret_cast<u32x4 *>(const_cast<void *>(col < cols ? c.k : c.v));
+    const int unit0 = col % cols * col_units;
+    walk_down(plane, row0, row_units, unit0, min(col_units, row_units - unit0), list, first, kept);
+    return;
+  }
+  col -= 2 * cols;
+  const int scale_cols = (scale_units + kMoveThreads - 1) / kMoveThreads;
+  if (col < 2 * scale_cols) {
+    SCALE *plane = reinterpret_cast<SCALE *>(const_cast<uint8_t *>(col < scale_cols ? c.ks : c.vs));
+    const int unit0 = col % scale_cols * kMoveThreads;
+    walk_down(plane, row0, scale_units, unit0, min(kMoveThreads, scale_units - unit0), list, first, kept);
+    return;
+  }
+  walk_down(c.row_weight, row0, 1, 0, 1, list, first, kept);
+  if (c.keep_idx != nullptr)
+    for (int j = threadIdx.x; j < kept; j += kMoveThreads) c.keep_idx[row0 + j] = list[j];
+  if (threadIdx.x == 0) c.cache_len[b] = kept;
+}
+
+template <typename SCALE>
+static void launch_moves(const EvictCall &c, const EvictWs &ws, int row_units, int scale_units, hipStream_t stream) {
+  if (c.k_out != nullptr) {
+    const long units = static_cast<long>(c.max_rows) * row_units;
+    const long chunks = std::max(1L, std::min((units + kMoveThreads * kMoveUnroll - 1) / (kMoveThreads * kMoveUnroll),
+                                              std::max(16L, 4096L / c.batch)));
+    move_kernel<SCALE><<<dim3(chunks, c.batch), dim3(kMoveThreads), 0, stream>>>(c, ws, row_units, scale_units);
+  } else {
+    const int col_units = 4;   // 64 bytes
+    const int cols = (row_units + col_units - 1) / col_units, scale_cols = (scale_units + kMoveThreads - 1) / kMoveThreads;
+    move_in_place_kernel<SCALE><<<dim3(2 * cols + 2 * scale_cols + 1, c.batch), dim3(kMoveThreads), 0, stream>>>(
+        c, ws, row_units, col_units, scale_units);
+  }
+}
+
+hipError_t launch_evict(const EvictCall &c, const EvictWs &ws, int Hkv, int D, hipStream_t stream) {
+  select_kernel<<<dim3(c.batch), dim3(kSelectThreads), 0, stream>>>(c, ws);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const bool q4 = c.ks != nullptr;
+  const int row_units = Hkv * D / (q4 ? 32 : 8);   // of 16 bytes
+  if (D == 128) launch_moves<uint32_t>(c, ws, row_units, q4 ? Hkv : 0, stream);
+  else launch_moves<uint16_t>(c, ws, row_units, q4 ? Hkv : 0, stream);
+  return hipGetLastError();
+}
+
+}  // namespace sonic

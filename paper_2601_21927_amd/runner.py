@@ -58,6 +58,7 @@ class SonicBatch:
         ws = sonic.prefill_workspace_bytes(self.batch, self.total_tokens, max(self.Hq, 1), self.Hkv, self.d)
         self.prefill_ws = torch.empty(max(ws, 256), dtype=torch.uint8, device=self.device)
         self.cache = None
+        self.cache_q4 = None
 
     # ------------------------------------------------------------- step 1
     def prefill(self, stream=None, nexus_scope: int = sonic.NEXUS_ALL, nexus_mass=None, key_weight=None) -> int:
@@ -77,6 +78,17 @@ class SonicBatch:
         c = self.cache
         return sonic.kv_compact(self.cu, self.role, self.k, self.v, c.k, c.v, c.row_off, c.row_cap, c.length,
                                 c.keep_idx, self.status, self.max_seqlen, stream=stream)
+
+    def alloc_cache_q4(self, capacities: Sequence[int]):
+        cap = np.asarray(capacities, dtype=np.int64)
+        off = np.concatenate([[0], np.cumsum(cap)[:-1]]).astype(np.int64)
+        self.cache_q4 = Q4Cache(int(cap.sum()), self.Hkv, self.d, off, cap.astype(np.int32), self.device)
+        return self.cache_q4
+
+    def compact_q4(self, stream=None) -> int:
+        c = self.cache_q4
+        return sonic.kv_compact_q4(self.cu, self.role, self.k, self.v, c.k, c.k_scale, c.v, c.v_scale, c.row_off, c.row_cap,
+                                   c.length, c.keep_idx, self.status, self.max_seqlen, stream=stream)
 
     def read_status(self) -> int:
         return int(self.status.item())
@@ -102,6 +114,9 @@ class CompactCache:
         self.batch = len(row_cap)
         self.ws = None
         self.ws_key = None
+        self.row_weight = None
+        self.weighted_ws = None
+        self.weighted_ws_key = None
 
     def decode(self, q, k_new, v_new, out, status, max_ctx: int, row_role: Optional[torch.Tensor] = None,
                stream=None) -> int:
@@ -114,3 +129,68 @@ class CompactCache:
             self.ws_key = key
         return sonic.compressed_decode(self.k, self.v, self.row_off, self.row_cap, self.length, q, k_new, v_new,
                                        out, self.ws, status, max_ctx, row_role=row_role, stream=stream)
+
+    def decode_weighted(self, q, k_new, v_new, out, status, max_ctx: int, stream=None) -> int:
+        """decode that also adds each row's attention to row_weight."""
+        B, Hq, d = q.shape
+        key = (B, Hq, d, int(max_ctx))
+        if self.row_weight is None:
+            self.row_weight = torch.zeros(self.k.shape[0], dtype=torch.float32, device=q.device)
+        if self.weighted_ws_key != key:
+            n = sonic.decode_weighted_workspace_bytes(B, Hq, d, int(max_ctx))
+            self.weighted_ws = torch.zeros(n, dtype=torch.uint8, device=q.device)   # counters start at zero
+            self.weighted_ws_key = key
+        return sonic.compressed_decode_weighted(self.k, self.v, self.row_off, self.row_cap, self.length, q, k_new, v_new, out,
+                                                self.row_weight, self.weighted_ws, status, max_ctx, stream=stream)
+
+    def evict(self, keep_head, keep_tail, budget, status, stream=None) -> int:
+        """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device."""
+        n = int(self.row_cap_host.max()) if self.batch else 0
+        ws = torch.empty(sonic.cache_evict_workspace_bytes(self.batch, n), dtype=torch.uint8, device=self.k.device)
+        return sonic.cache_evict(self.k, self.v, self.row_off, self.length, self.row_weight, keep_head, keep_tail, budget, ws,
+                                 status, n, stream=stream)
+
+
+class Q4Cache:
+    """The same rows in 4 bits: codes [rows, Hkv, d / 2] and scale bytes [rows, Hkv, d / 32] of K and V."""
+
+    def __init__(self, rows, Hkv, d, row_off, row_cap, device):
+        self.rows, self.Hkv, self.d = rows, Hkv, d
+        n = max(rows, 1)
+
+        def plane(width):
+            return torch.full((n, Hkv, width), 255, dtype=torch.uint8, device=device)   # NaN until written
+
+        self.k, self.k_scale, self.v, self.v_scale = plane(d // 2), plane(d // 32), plane(d // 2), plane(d // 32)
+        self.keep_idx = torch.full((n,), -1, dtype=torch.int32, device=device)
+        self.row_weight = torch.zeros(n, dtype=torch.float32, device=device)
+        self.row_off_host = np.asarray(row_off, dtype=np.int64)
+        self.row_cap_host = np.asarray(row_cap, dtype=np.int32)
+        self.row_off = torch.from_numpy(self.row_off_host).to(device)
+        self.row_cap = torch.from_numpy(self.row_cap_host).to(device)
+        self.length = torch.zeros(len(row_cap), dtype=torch.int32, device=device)
+        self.batch = len(row_cap)
+        self.ws = None
+        self.ws_key = None
+
+    def decode(self, q, k_new, v_new, out, status, max_ctx: int, weighted: bool = False, stream=None) -> int:
+        B, Hq, d = q.shape
+        key = (B, Hq, d, int(max_ctx), weighted)
+        if self.ws_key != key:
+            n = sonic.decode_q4_workspace_bytes(B, Hq, d, int(max_ctx), weighted)
+            self.ws = torch.zeros(n, dtype=torch.uint8, device=q.device)   # counters start at zero
+            self.ws_key = key
+        return sonic.compressed_decode_q4(self.k, self.k_scale, self.v, self.v_scale, self.row_off, self.row_cap, self.length, q,
+                                          k_new, v_new, out, self.ws, status, max_ctx,
+                                          row_weight=self.row_weight if weighted else None, stream=stream)
+
+    def expand(self, row_begin, row_end, k, v, out_row_off, out_row_cap, status, max_rows: int, stream=None) -> int:
+        return sonic.cache_expand_q4(self.k, self.k_scale, self.v, self.v_scale, self.row_off, self.row_cap, row_begin, row_end, k,
+                                     v, out_row_off, out_row_cap, status, max_rows, stream=stream)
+
+    def evict(self, keep_head, keep_tail, budget, status, stream=None) -> int:
+        """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device."""
+        n = int(self.row_cap_host.max()) if self.batch else 0
+        ws = torch.empty(sonic.cache_evict_workspace_bytes(self.batch, n), dtype=torch.uint8, device=self.k.device)
+        return sonic.cache_evict(self.k, self.v, self.row_off, self.length, self.row_weight, keep_head, keep_tail, budget, ws,
+                                 status, n, k_scale=self.k_scale, v_scale=self.v_scale, stream=stream)

@@ -35,6 +35,9 @@ EXPORTS = (
     "sonic_nexus_extend_workspace_bytes",
     "sonic_nexus_extend", "sonic_role_projection_workspace_bytes", "sonic_role_projection",
     "sonic_nexus_recon_workspace_bytes", "sonic_nexus_recon_targets",
+    "sonic_kv_compact_q4", "sonic_cache_expand_q4", "sonic_decode_q4_workspace_bytes", "sonic_compressed_decode_q4",
+    "sonic_decode_weighted_workspace_bytes", "sonic_compressed_decode_weighted", "sonic_kv_compact_weights",
+    "sonic_cache_evict_workspace_bytes", "sonic_cache_evict",
 )
 
 _lib = None
@@ -92,6 +95,24 @@ def lib() -> ctypes.CDLL:
     L.sonic_nexus_recon_workspace_bytes.argtypes = [_i32, _i32]
     L.sonic_nexus_recon_targets.restype = _i32
     L.sonic_nexus_recon_targets.argtypes = [_i32, _i32, _i32, _p, _p, _p, _p, _i32, _p, _p, _p, _p, _sz, _p, _p]
+    L.sonic_kv_compact_q4.restype = _i32
+    L.sonic_kv_compact_q4.argtypes = [_i32] * 5 + [_p] * 14
+    L.sonic_cache_expand_q4.restype = _i32
+    L.sonic_cache_expand_q4.argtypes = [_i32] * 4 + [_p] * 14
+    L.sonic_decode_q4_workspace_bytes.restype = _sz
+    L.sonic_decode_q4_workspace_bytes.argtypes = [_i32] * 5
+    L.sonic_compressed_decode_q4.restype = _i32
+    L.sonic_compressed_decode_q4.argtypes = [_i32] * 5 + [_p] * 10 + [_f32, _p, _p, _p, _sz, _p, _p]
+    L.sonic_decode_weighted_workspace_bytes.restype = _sz
+    L.sonic_decode_weighted_workspace_bytes.argtypes = [_i32] * 4
+    L.sonic_compressed_decode_weighted.restype = _i32
+    L.sonic_compressed_decode_weighted.argtypes = [_i32] * 5 + [_p] * 8 + [_f32, _p, _p, _p, _sz, _p, _p]
+    L.sonic_kv_compact_weights.restype = _i32
+    L.sonic_kv_compact_weights.argtypes = [_i32] * 3 + [_p] * 8
+    L.sonic_cache_evict_workspace_bytes.restype = _sz
+    L.sonic_cache_evict_workspace_bytes.argtypes = [_i32] * 2
+    L.sonic_cache_evict.restype = _i32
+    L.sonic_cache_evict.argtypes = [_i32] * 4 + [_p] * 20 + [_sz, _p, _p]
     _lib = L
     return L
 
@@ -309,3 +330,173 @@ def nexus_recon_targets(cu_seqlens, role, turn_id, h, target, cos_target, entrop
         cu_seqlens.numel() - 1, T, Dm, _ptr(cu_seqlens), _ptr(role), _ptr(turn_id), _ptr(h), n, _ptr(target),
         _ptr(cos_target), _ptr(entropy_ratio), _ptr(workspace), workspace.numel() * workspace.element_size(),
         _ptr(dev_status), _stream(stream)))
+
+
+# ----------------------------------------------------------------- 4-bit rows
+def _on_one_device(*ts):
+    """The device of the call's tensors: a call with tensors of two GPUs is refused, and one whose tensors are not
+    on the current GPU is made on theirs."""
+    _dev(*ts)
+    devs = {t.device for t in ts if t is not None}
+    if len(devs) != 1:
+        raise ValueError("tensors of one call must be on one GPU")
+    return torch.cuda.device(devs.pop())
+
+
+def _shapes(where, **named):
+    """named=(tensor, shape): a None in a shape stands for any size."""
+    for name, (t, shape) in named.items():
+        if t is not None and (t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape))):
+            raise ValueError(f"{where}: {name} must be {shape}, got {tuple(t.shape)}")
+
+
+def _q4_rows(where, Hkv, d, k_cache, k_scale, v_cache, v_scale):
+    _types(k_cache=(k_cache, _U8), k_scale=(k_scale, _U8), v_cache=(v_cache, _U8), v_scale=(v_scale, _U8))
+    rows = k_cache.shape[0]
+    _shapes(where, k_cache=(k_cache, (rows, Hkv, d // 2)), v_cache=(v_cache, (rows, Hkv, d // 2)),
+            k_scale=(k_scale, (rows, Hkv, d // 32)), v_scale=(v_scale, (rows, Hkv, d // 32)))
+
+
+def kv_compact_q4(cu_seqlens, role, k, v, k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, cache_len, keep_idx,
+                  dev_status, max_seqlen: int, stream=None) -> int:
+    """kv_compact into 4-bit rows: k_cache/v_cache uint8 [rows,Hkv,d/2] codes, k_scale/v_scale uint8 [rows,Hkv,d/32]."""
+    with _on_one_device(cu_seqlens, role, k, v, k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, cache_len, keep_idx,
+                        dev_status):
+        T, Hkv, d = k.shape
+        B = cu_seqlens.numel() - 1
+        _q4_rows("kv_compact_q4", Hkv, d, k_cache, k_scale, v_cache, v_scale)
+        _types(cu_seqlens=(cu_seqlens, _I32), role=(role, _U8), k=(k, _BF16), v=(v, _BF16), cache_row_off=(cache_row_off, _I64),
+               cache_row_cap=(cache_row_cap, _I32), cache_len=(cache_len, _I32), keep_idx=(keep_idx, _I32),
+               dev_status=(dev_status, _I32))
+        _shapes("kv_compact_q4", role=(role, (T,)), v=(v, (T, Hkv, d)), cache_row_off=(cache_row_off, (B,)),
+                cache_row_cap=(cache_row_cap, (B,)), cache_len=(cache_len, (B,)), keep_idx=(keep_idx, (k_cache.shape[0],)))
+        return int(lib().sonic_kv_compact_q4(
+            B, T, int(max_seqlen), Hkv, d, _ptr(cu_seqlens), _ptr(role), _ptr(k), _ptr(v), _ptr(k_cache), _ptr(k_scale), _ptr(v_cache),
+            _ptr(v_scale), _ptr(cache_row_off), _ptr(cache_row_cap), _ptr(cache_len), _ptr(keep_idx), _ptr(dev_status),
+            _stream(stream)))
+
+
+def cache_expand_q4(k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, row_begin, row_end, k, v, out_row_off,
+                    out_row_cap, dev_status, max_rows: int, stream=None) -> int:
+    """4-bit rows row_begin[b] .. row_end[b] of every request to rows out_row_off[b] .. of k/v [n,Hkv,d] bf16."""
+    with _on_one_device(k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, row_begin, row_end, k, v, out_row_off,
+                        out_row_cap, dev_status):
+        _, Hkv, d = k.shape
+        B = cache_row_off.numel()
+        _q4_rows("cache_expand_q4", Hkv, d, k_cache, k_scale, v_cache, v_scale)
+        _types(cache_row_off=(cache_row_off, _I64), cache_row_cap=(cache_row_cap, _I32), row_begin=(row_begin, _I32),
+               row_end=(row_end, _I32), k=(k, _BF16), v=(v, _BF16), out_row_off=(out_row_off, _I64),
+               out_row_cap=(out_row_cap, _I32), dev_status=(dev_status, _I32))
+        _shapes("cache_expand_q4", v=(v, tuple(k.shape)), cache_row_cap=(cache_row_cap, (B,)), row_begin=(row_begin, (B,)),
+                row_end=(row_end, (B,)), out_row_off=(out_row_off, (B,)), out_row_cap=(out_row_cap, (B,)))
+        return int(lib().sonic_cache_expand_q4(
+            B, int(max_rows), Hkv, d, _ptr(k_cache), _ptr(k_scale), _ptr(v_cache), _ptr(v_scale), _ptr(cache_row_off),
+            _ptr(cache_row_cap), _ptr(row_begin), _ptr(row_end), _ptr(k), _ptr(v), _ptr(out_row_off), _ptr(out_row_cap),
+            _ptr(dev_status), _stream(stream)))
+
+
+def decode_q4_workspace_bytes(batch: int, num_q_heads: int, head_dim: int, max_ctx: int, weighted: bool) -> int:
+    return int(lib().sonic_decode_q4_workspace_bytes(batch, num_q_heads, head_dim, max_ctx, int(bool(weighted))))
+
+
+def compressed_decode_q4(k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, workspace,
+                         dev_status, max_ctx: int, row_weight=None, softmax_scale=None, stream=None) -> int:
+    """compressed_decode over 4-bit rows; row_weight fp32 [rows] or None: each row's attention is added to it."""
+    with _on_one_device(k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, workspace,
+                        dev_status, row_weight):
+        B, Hq, d = q.shape
+        Hkv = k_new.shape[1]
+        _q4_rows("compressed_decode_q4", Hkv, d, k_cache, k_scale, v_cache, v_scale)
+        _decode_args("compressed_decode_q4", B, Hq, Hkv, d, k_cache.shape[0], cache_row_off, cache_row_cap, cache_len, q, k_new, v_new,
+                     out, dev_status, row_weight)
+        scale = 0.0 if softmax_scale is None else float(softmax_scale)   # 0: the library's 1/sqrt(d)
+        return int(lib().sonic_compressed_decode_q4(
+            B, Hq, Hkv, d, int(max_ctx), _ptr(k_cache), _ptr(k_scale), _ptr(v_cache), _ptr(v_scale), _ptr(cache_row_off),
+            _ptr(cache_row_cap), _ptr(cache_len), _ptr(q), _ptr(k_new), _ptr(v_new), scale, _ptr(out), _ptr(row_weight),
+            _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream)))
+
+
+def _decode_args(where, B, Hq, Hkv, d, rows, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, dev_status, row_weight):
+    _types(cache_row_off=(cache_row_off, _I64), cache_row_cap=(cache_row_cap, _I32), cache_len=(cache_len, _I32), q=(q, _BF16),
+           k_new=(k_new, _BF16), v_new=(v_new, _BF16), out=(out, _F32), dev_status=(dev_status, _I32), row_weight=(row_weight, _F32))
+    _shapes(where, k_new=(k_new, (B, Hkv, d)), v_new=(v_new, (B, Hkv, d)), out=(out, (B, Hq, d)), cache_row_off=(cache_row_off, (B,)),
+            cache_row_cap=(cache_row_cap, (B,)), cache_len=(cache_len, (B,)), row_weight=(row_weight, (rows,)))
+
+
+# ----------------------------------------------------------------- row weights, eviction
+def decode_weighted_workspace_bytes(batch: int, num_q_heads: int, head_dim: int, max_ctx: int) -> int:
+    return int(lib().sonic_decode_weighted_workspace_bytes(batch, num_q_heads, head_dim, max_ctx))
+
+
+def compressed_decode_weighted(k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, row_weight, workspace,
+                               dev_status, max_ctx: int, softmax_scale=None, stream=None) -> int:
+    """compressed_decode that also adds each row's attention, averaged over the q-heads, to row_weight fp32 [rows]."""
+    with _on_one_device(k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, row_weight, workspace,
+                        dev_status):
+        B, Hq, d = q.shape
+        Hkv = k_new.shape[1]
+        rows = k_cache.shape[0]
+        _types(k_cache=(k_cache, _BF16), v_cache=(v_cache, _BF16))
+        _shapes("compressed_decode_weighted", k_cache=(k_cache, (rows, Hkv, d)), v_cache=(v_cache, (rows, Hkv, d)))
+        _decode_args("compressed_decode_weighted", B, Hq, Hkv, d, rows, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out,
+                     dev_status, row_weight)
+        scale = 0.0 if softmax_scale is None else float(softmax_scale)   # 0: the library's 1/sqrt(d)
+        return int(lib().sonic_compressed_decode_weighted(
+            B, Hq, Hkv, d, int(max_ctx), _ptr(k_cache), _ptr(v_cache), _ptr(cache_row_off), _ptr(cache_row_cap), _ptr(cache_len),
+            _ptr(q), _ptr(k_new), _ptr(v_new), scale, _ptr(out), _ptr(row_weight), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream)))
+
+
+def kv_compact_weights(cu_seqlens, key_weight, cache_row_off, cache_len, keep_idx, row_weight, dev_status, max_rows: int,
+                       stream=None) -> int:
+    """The prefill's key_weight fp32 [T] to the rows a compaction kept: row_weight fp32 [rows], keep_idx int32 [rows]."""
+    with _on_one_device(cu_seqlens, key_weight, cache_row_off, cache_len, keep_idx, row_weight, dev_status):
+        B = cu_seqlens.numel() - 1
+        _types(cu_seqlens=(cu_seqlens, _I32), key_weight=(key_weight, _F32), cache_row_off=(cache_row_off, _I64),
+               cache_len=(cache_len, _I32), keep_idx=(keep_idx, _I32), row_weight=(row_weight, _F32), dev_status=(dev_status, _I32))
+        _shapes("kv_compact_weights", key_weight=(key_weight, (None,)), cache_row_off=(cache_row_off, (B,)),
+                cache_len=(cache_len, (B,)), keep_idx=(keep_idx, tuple(row_weight.shape)))
+        return int(lib().sonic_kv_compact_weights(
+            B, key_weight.numel(), int(max_rows), _ptr(cu_seqlens), _ptr(key_weight), _ptr(cache_row_off), _ptr(cache_len),
+            _ptr(keep_idx), _ptr(row_weight), _ptr(dev_status), _stream(stream)))
+
+
+def cache_evict_workspace_bytes(batch: int, max_rows: int) -> int:
+    return int(lib().sonic_cache_evict_workspace_bytes(batch, max_rows))
+
+
+def cache_evict(k_cache, v_cache, cache_row_off, cache_len, row_weight, keep_head, keep_tail, budget, workspace, dev_status,
+                max_rows: int, k_scale=None, v_scale=None, k_out=None, v_out=None, k_scale_out=None, v_scale_out=None,
+                out_row_off=None, out_row_cap=None, out_len=None, out_weight=None, keep_idx=None, stream=None) -> int:
+    """Keep the first keep_head[b], the last keep_tail[b] and the heaviest other rows, budget[b] in all.  bf16 rows
+    [rows,Hkv,d], or codes [rows,Hkv,d/2] with k_scale/v_scale [rows,Hkv,d/32].  Without k_out the rows move down in
+    place; with it (and v_out, the scales, out_row_off, out_row_cap, out_len, out_weight) they go to another cache.
+    keep_idx int32 [rows of the cache written] or None: the kept rows' places before the call."""
+    with _on_one_device(k_cache, v_cache, cache_row_off, cache_len, row_weight, keep_head, keep_tail, budget, workspace, dev_status,
+                        k_scale, v_scale, k_out, v_out, k_scale_out, v_scale_out, out_row_off, out_row_cap, out_len, out_weight,
+                        keep_idx):
+        rows, Hkv, width = k_cache.shape
+        B = cache_row_off.numel()
+        if k_scale is None:
+            d = width
+            _types(k_cache=(k_cache, _BF16), v_cache=(v_cache, _BF16), k_out=(k_out, _BF16), v_out=(v_out, _BF16))
+            _shapes("cache_evict", v_cache=(v_cache, (rows, Hkv, d)))
+        else:
+            d = 2 * width
+            _q4_rows("cache_evict", Hkv, d, k_cache, k_scale, v_cache, v_scale)
+            _types(k_out=(k_out, _U8), v_out=(v_out, _U8), k_scale_out=(k_scale_out, _U8), v_scale_out=(v_scale_out, _U8))
+        n = rows if k_out is None else k_out.shape[0]
+        _types(cache_row_off=(cache_row_off, _I64), cache_len=(cache_len, _I32), row_weight=(row_weight, _F32),
+               keep_head=(keep_head, _I32), keep_tail=(keep_tail, _I32), budget=(budget, _I32), out_row_off=(out_row_off, _I64),
+               out_row_cap=(out_row_cap, _I32), out_len=(out_len, _I32), out_weight=(out_weight, _F32), keep_idx=(keep_idx, _I32),
+               dev_status=(dev_status, _I32))
+        _shapes("cache_evict", row_weight=(row_weight, (rows,)), cache_len=(cache_len, (B,)), keep_head=(keep_head, (B,)),
+                keep_tail=(keep_tail, (B,)), budget=(budget, (B,)), k_out=(k_out, (n, Hkv, width)), v_out=(v_out, (n, Hkv, width)),
+                k_scale_out=(k_scale_out, (n, Hkv, d // 32)), v_scale_out=(v_scale_out, (n, Hkv, d // 32)),
+                out_row_off=(out_row_off, (B,)), out_row_cap=(out_row_cap, (B,)), out_len=(out_len, (B,)),
+                out_weight=(out_weight, (n,)), keep_idx=(keep_idx, (n,)))
+        return int(lib().sonic_cache_evict(
+            B, int(max_rows), Hkv, d, _ptr(k_cache), _ptr(k_scale), _ptr(v_cache), _ptr(v_scale), _ptr(cache_row_off), _ptr(cache_len),
+            _ptr(row_weight), _ptr(keep_head), _ptr(keep_tail), _ptr(budget), _ptr(k_out), _ptr(k_scale_out), _ptr(v_out),
+            _ptr(v_scale_out), _ptr(out_row_off), _ptr(out_row_cap), _ptr(out_len), _ptr(out_weight), _ptr(keep_idx), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream)))
