@@ -44,6 +44,7 @@ hipError_t launch_compact(int batch, int total_tokens, int max_seqlen, int Hkv, 
                           const int32_t *row_cap, int32_t *cache_len, int32_t *keep_idx, int32_t *status,
                           hipStream_t stream);
 DecodeShape decode_shape(int batch, int Hkv, int G, int D, int max_ctx, bool masked, size_t part_bytes);
+DecodeShape decode_shape_q4(int batch, int Hkv, int G, int D, int max_ctx);
 size_t decode_ws_layout(int batch, int Hkv, size_t part_bytes, DecodeWs *ws, char *base);
 size_t decode_scratch_layout(int batch, int Hkv, size_t part_bytes, DecodeWs *ws, char *base);
 hipError_t decode_scratch(hipStream_t stream, char **base);
@@ -706,7 +707,12 @@ size_t sonic_decode_weighted_workspace_bytes(int32_t batch, int32_t Hq, int32_t 
 }
 
 size_t sonic_decode_q4_workspace_bytes(int32_t batch, int32_t Hq, int32_t d, int32_t max_ctx, int32_t weighted) {
-  return weighted ? sonic_decode_weighted_workspace_bytes(batch, Hq, d, max_ctx) : sonic_decode_workspace_bytes(batch, Hq, d, max_ctx);
+  if (batch <= 0 || Hq <= 0 || max_ctx <= 0) return 256;
+  size_t part = 0;   // for any kv-head count, as above
+  for (int hkv = 1; hkv <= Hq; ++hkv)
+    if (Hq % hkv == 0 && Hq / hkv <= 8) part = std::max(part, decode_shape_q4(batch, hkv, Hq / hkv, d, max_ctx).part_bytes);
+  return align_up(align_up(decode_counter_bytes(batch, Hq) + part, 256) +
+                      (weighted ? weighted_ws_layout(batch, Hq, max_ctx, nullptr, nullptr) : 0), 256);
 }
 
 int32_t sonic_compressed_decode_weighted(int32_t batch, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_ctx, void *k_cache,
@@ -749,7 +755,7 @@ int32_t sonic_compressed_decode_q4(int32_t batch, int32_t Hq, int32_t Hkv, int32
       !aligned(workspace, 256))
     return SONIC_ERR_INVALID_ARG;
   if (workspace_bytes < sonic_decode_q4_workspace_bytes(batch, Hq, d, max_ctx, row_weight != nullptr)) return SONIC_ERR_WORKSPACE;
-  const DecodeShape sh = decode_shape(batch, Hkv, Hq / Hkv, d, max_ctx, false, SIZE_MAX);
+  const DecodeShape sh = decode_shape_q4(batch, Hkv, Hq / Hkv, d, max_ctx);
   char *base = static_cast<char *>(workspace);
   DecodeWs ws;
   decode_ws_layout(batch, Hkv, sh.part_bytes, &ws, base);

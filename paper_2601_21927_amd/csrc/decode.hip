@@ -68,6 +68,38 @@ DecodeShape decode_shape(int batch, int Hkv, int G, int D, int max_ctx, bool mas
   return sh;
 }
 
+// The same for 4-bit rows.  A row is a quarter of the bytes, so a call is sooner short of work than of bandwidth: ranges
+// are longer and waves fewer.  Times of a step, 32 / 8 heads of 128.
+// - Fewer than 256 pairs: about as many ranges as give every CU a workgroup, of 256 rows and more, and one up to 448 rows
+//   (the hand-over between workgroups costs 1.3 us of 6.8: 8 requests of 100 rows, one range and two; 400 rows, one range
+//   8.8 us and four 8.7; 1,328 rows, two ranges 11.8, four 10.0, eight 11.7; one request of 8,000 rows, 16 ranges 11.2
+//   and 32 11.8, and of 100,001 rows, 16 ranges 44 and 32 30).
+// - Four waves up to 512 rows a range, eight above, which keep more loads in flight and divide the work finer
+//   (8 requests of 1,328 rows in four ranges, four waves 10.0 and eight 10.4; of 4,000 rows 14.6 and 14.1; 24 of 4,000
+//   rows in one range 30.3 and 26.4).
+// - 256 pairs and more with long contexts share the rows evenly (see decode_shape) among 1,024 workgroups of four waves,
+//   all of them resident: 64 of 180 .. 4,300 rows 36.7 us, with 768 workgroups 39.9, 1,536 38.1 and a range
+//   per pair and 512 rows 39.
+DecodeShape decode_shape_q4(int batch, int Hkv, int G, int D, int max_ctx) {
+  DecodeShape sh{1, 0, 4, 0};
+  const long pairs = static_cast<long>(batch) * Hkv;
+  long slots = pairs;
+  if (pairs >= 256 && pairs < 1024 && batch <= kWave && max_ctx >= 2048) {
+    sh.target = static_cast<int>(std::max(1024L / Hkv, static_cast<long>(batch)));   // (a request takes one at least)
+    sh.splits = sh.target + (batch + 15) / 16;
+    slots = static_cast<long>(sh.splits) * Hkv;
+  } else {
+    const long by_rows = max_ctx <= 448 ? 1 : (static_cast<long>(max_ctx) + 255) / 256;
+    long most = 256 / pairs;
+    if (most > kMaxSplits && max_ctx < 512L * most) most = kMaxSplits;
+    sh.splits = static_cast<int>(std::max(1L, std::min({most, by_rows, static_cast<long>(kMaxSplitsQ4)})));
+    slots = pairs * sh.splits;
+    if (max_ctx > 512L * sh.splits) sh.waves = 8;
+  }
+  sh.part_bytes = sh.splits > 1 ? static_cast<size_t>(slots) * G * (D + 2) * sizeof(float) : 0;
+  return sh;
+}
+
 // Fixed layout of a scratch array shared by calls of different shapes: the counters
 // sit at the same offsets for every call (each call leaves them at zero), the partial
 // records after them.  Returns the bytes a call needs, or 0 when its requests or

@@ -57,13 +57,14 @@ constexpr int kStopBit = 1 << 30;
 // contexts of 3,000 .. 8,000 rows, 326 us so and 264 alternating.  Shorter rows are better
 // off with a head at a time (32 / 8, 64 contexts of 100 .. 4,000, 52.6 and 55.5).
 constexpr int kLongRow = 4096;
-template <int D, bool Q4> __host__ __device__ constexpr int row_bytes(int Hkv) { return Hkv * D * 2 / (Q4 ? 4 : 1); }
 constexpr int kMaxSplits = 16;   // of a (request, kv-head): the merge loads all its partials in one round trip
+constexpr int kMaxSplitsQ4 = 64; // 4-bit rows, four round trips at most: their contexts are short of work, not of bytes
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16_t;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+#define SONIC_GLOBAL __attribute__((address_space(1)))   // a pointer made from an integer is a generic one, and slower, without
 
 // The K/V loads of the pipeline go straight to LDS and are written as inline
 // assembly, so the compiler does not count them (it would otherwise wait for the
@@ -97,7 +98,7 @@ __device__ __forceinline__ bool stops(int32_t pending) {
 }
 
 template <int D, int G, bool MASKED, int NW, bool BAL, bool Q4, bool SCORED>
-__global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
+__global__ __launch_bounds__(NW * kWave, Q4 ? 4 : 2) void decode_kernel(
     uint16_t *__restrict__ kc, uint16_t *__restrict__ vc, const int64_t *__restrict__ row_off,
     const int32_t *__restrict__ row_cap, int32_t *__restrict__ cache_len, const uint8_t *__restrict__ row_role,
     const uint16_t *__restrict__ q, const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new,
@@ -115,8 +116,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
   static_assert(NI * kWave == kGroupRows * DC, "a group's rows are whole DMA instructions");
   // ring: [wave][slot 0/1][K, V][16 rows][D] with the swizzles above (K for the
   // row-fragment reads of the scores, V for the transposing reads); reused for the
-  // merge of the waves at the end.  4-bit rows: [wave][16 rows][D], one group's V as bf16
-  constexpr int RING = Q4 ? (SLOT > 2 * G * DP ? SLOT : 2 * G * DP) : 4 * SLOT;
+  // merge of the waves at the end.  4-bit rows: [wave][32 rows][D], one block's V as bf16
+  constexpr int RING = Q4 ? (2 * SLOT > 2 * G * DP ? 2 * SLOT : 2 * G * DP) : 4 * SLOT;
   __shared__ __align__(16) uint16_t ring[NW * RING];
   // each wave's copy of the G query rows (direct-to-LDS, so that no load the
   // compiler counts precedes the pipeline's)
@@ -133,12 +134,18 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
   static_assert(!MASKED || (!Q4 && !SCORED), "the masked cache is a bf16 one without weights");
 
   // BAL: blockIdx.z == 0, the grid is (workgroups, kv-heads) or, with long rows, (kv-heads, workgroups)
-  const bool heads_first = BAL && row_bytes<D, Q4>(Hkv) >= kLongRow;
-  const int kvh = heads_first ? blockIdx.x : blockIdx.y;
+  const bool heads_first = BAL && !Q4 && Hkv * D * 2 >= kLongRow;
+  // 4-bit rows: blockIdx.x alone.  The kv-heads of one range of rows are neighbours on one XCD (workgroup i goes to XCD
+  // i % 8): a head's row is 64 bytes of codes and 4 of scales, and the lines they share, and the memory pages, are
+  // wanted at about the same time.
+  const int unit = Q4 ? blockIdx.x / (kNumXcd * Hkv) * kNumXcd + blockIdx.x % kNumXcd : 0;   // of ranges
+  const int kvh = Q4 ? blockIdx.x / kNumXcd % Hkv : heads_first ? blockIdx.x : blockIdx.y;
+  if (Q4 && unit >= (BAL ? nsplit_max : nsplit_max * batch)) return;   // the grid is whole rows of XCDs
+  const bool first_group = blockIdx.x == 0 && (Q4 || blockIdx.y == 0);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = threadIdx.x % kWave;
   const int Hq = Hkv * G;
-  const int nsplit = heads_first ? gridDim.y : gridDim.x;   // BAL: workgroups of a kv-head
+  const int nsplit = Q4 ? nsplit_max : heads_first ? gridDim.y : gridDim.x;   // BAL: workgroups of a kv-head
   int split, b, nsp, R, len;
   int64_t base;
   // A pending error other than a capacity error (a layout error of an earlier call) stops
@@ -162,7 +169,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
     const int64_t lo = row_off[lb];
     stop = stops(pending);
     const bool fits = ll >= 0 && ll < lc && ll < max_ctx;   // (behind an error a length may be anything)
-    if (__any(!fits) && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) raise_status(status, SONIC_ERR_CAPACITY);
+    if (__any(!fits) && first_group && threadIdx.x == 0) raise_status(status, SONIC_ERR_CAPACITY);
     lane_ctx = l < batch && fits ? ll + 1 : 0;
     const int groups = (lane_ctx + kGroupRows - 1) / kGroupRows;
     const int total = __builtin_amdgcn_readlane(wave_scan(groups), kWave - 1);
@@ -173,7 +180,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
                   max(__builtin_amdgcn_readlane(longest, 32), __builtin_amdgcn_readlane(longest, 48)));
     const unsigned ug = groups;
     const int active = __popcll(__ballot(lane_ctx > 0));
-    int rg = max(max(256 / kGroupRows, (longest + kMaxSplits - 1) / kMaxSplits), (total + target - 1) / target);
+    constexpr int MOST = Q4 ? kMaxSplitsQ4 : kMaxSplits;
+    int rg = max(max(256 / kGroupRows, (longest + MOST - 1) / MOST), (total + target - 1) / target);
     int mine, upto;
     auto cut = [&](int groups_each) {
       rg = groups_each;
@@ -189,9 +197,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
       int most = longest;
       if (nsplit > active) most = min(most, (total + nsplit - active - 1) / (nsplit - active));
 #pragma unroll 1
-      for (int i = 0; used > nsplit; ++i) cut(i < 4 ? min(most, half + half * i / 32) : most);
+      for (int i = 0; used > nsplit && i < 5; ++i) cut(i < 4 ? min(most, half + half * i / 32) : most);
     }
-    const int w = heads_first ? blockIdx.y : blockIdx.x;
+    const int w = Q4 ? unit : heads_first ? blockIdx.y : blockIdx.x;
     b = __popcll(__ballot(upto <= w));
     R = rg * kGroupRows;
     // The workgroups left without rows count for the active requests in turn, or, where there
@@ -200,7 +208,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
     const unsigned spare = nsplit - used;
     flat = spare * Hkv <= 128;
     if (active == 0) {   // no request has room: nothing to count or advance
-      if (SCORED && blockIdx.x == 0 && blockIdx.y == 0 && l < batch && threadIdx.x < kWave) rows.fresh[l] = 0;
+      if (SCORED && first_group && l < batch && threadIdx.x < kWave) rows.fresh[l] = 0;
       return;
     }
     counts = Hkv * (active + static_cast<int>(spare));
@@ -229,8 +237,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
     if (!flat) counts = __builtin_amdgcn_readlane(expect, b);
     call_counts = active;
   } else {
-    split = blockIdx.x;
-    b = blockIdx.z;
+    split = Q4 ? unit % nsplit_max : blockIdx.x;
+    b = Q4 ? unit / nsplit_max : blockIdx.z;
     // the status word, the length and the request's first cache row are requested
     // together (one round trip for all three)
     const int32_t pending = __hip_atomic_load(status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -256,8 +264,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
   float *orow = out + (static_cast<size_t>(b) * Hq + kvh * G) * D;
   // the pair's partials: [split][G][D] values, then, behind every pair's, [split][G] (max, sum)
   const size_t slot0 = BAL ? static_cast<size_t>(kvh) * nsplit + first : static_cast<size_t>(pair) * nsplit_max;
+  const size_t slots = Q4 ? static_cast<size_t>(nsplit_max) * Hkv * (BAL ? 1 : batch) : static_cast<size_t>(gridDim.x) * gridDim.y * gridDim.z;
   float *const acc_rec = ws.part + slot0 * (G * D);
-  float *const stat_rec = ws.part + static_cast<size_t>(gridDim.x) * gridDim.y * gridDim.z * (G * D) + slot0 * (2 * G);
+  float *const stat_rec = ws.part + slots * (G * D) + slot0 * (2 * G);
   // A pair's last workgroup counts the pair for its request in done[b]; the last pair of a
   // request advances its length.  BAL: a workgroup without rows counts for a request as well,
   // and a request's last count is one count of the call in the upper bits of done[0]; the
@@ -354,46 +363,67 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
     const int u = min(static_cast<int>(threadIdx.x), G * D / 4 - 1);
     const rsrc_t ra = partial_rsrc(acc_rec), rs = partial_rsrc(stat_rec);
     const int head = min(wave * (kWave / LH) + lane / 16, G - 1), sp = lane % 16;
-    const auto ml = __builtin_amdgcn_raw_buffer_load_b64(rs, (min(sp, nsp - 1) * G + head) * 8, 0, kSystemScope);
+    constexpr int ROUNDS = (Q4 ? kMaxSplitsQ4 : kMaxSplits) / kMaxSplits;   // of 16 splits each
+    u32x2 ml[ROUNDS];
+#pragma unroll
+    for (int c = 0; c < ROUNDS; ++c)
+      if (c == 0 || c * kMaxSplits < nsp)
+        ml[c] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, (min(c * kMaxSplits + sp, nsp - 1) * G + head) * 8, 0, kSystemScope));
     f32x4 a[kMaxSplits];
-    auto load = [&](auto n) {
+    auto load = [&](auto n, int from) {
 #pragma unroll
       for (int i = 0; i < decltype(n)::value; ++i)
-        a[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, u * 16, min(i, nsp - 1) * (G * D * 4), kSystemScope));
+        a[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, u * 16, min(from + i, nsp - 1) * (G * D * 4), kSystemScope));
     };
-    if (nsp <= 4) load(std::integral_constant<int, 4>{});
-    else load(std::integral_constant<int, kMaxSplits>{});
+    if (nsp <= 4) load(std::integral_constant<int, 4>{}, 0);
+    else load(std::integral_constant<int, kMaxSplits>{}, 0);
     __builtin_amdgcn_sched_barrier(0);
     // behind the loads, so that the round trips pass together (the compiler waits for an
     // atomic's result on the spot)
     int old_done = 0;
     if (threadIdx.x == 0) old_done = count(false);
-    const float m = sp < nsp ? __uint_as_float(ml[0]) : -INFINITY;
-    float top = m;
+    float m[ROUNDS], w[ROUNDS], top = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < ROUNDS; ++c) {
+      m[c] = c * kMaxSplits + sp < nsp ? __uint_as_float(ml[c][0]) : -INFINITY;
+      top = c == 0 ? m[c] : fmaxf(top, m[c]);
+    }
     top = fmaxf(top, row_rotate<8>(top));
     top = fmaxf(top, row_rotate<4>(top));
     top = fmaxf(top, row_rotate<2>(top));
     top = fmaxf(top, row_rotate<1>(top));
-    const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-    // (a range whose scores are all NaN has no maximum; its sum makes the kept normaliser NaN)
-    float sum = w == 0.f && !SCORED ? 0.f : w * __uint_as_float(ml[1]);
-    if constexpr (Q4 || SCORED) asm("" : "+v"(sum));   // (see soften)
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < ROUNDS; ++c) {
+      w[c] = m[c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[c] - top);
+      // (a range whose scores are all NaN has no maximum; its sum makes the kept normaliser NaN)
+      float part = w[c] == 0.f && !SCORED ? 0.f : w[c] * __uint_as_float(ml[c][1]);
+      if (c > 0 && c * kMaxSplits >= nsp) part = 0.f;
+      if constexpr (Q4 || SCORED) asm("" : "+v"(part));   // the rounded product, with and without weights
+      sum = c == 0 ? part : sum + part;
+    }
     sum += row_rotate<8>(sum);
     sum += row_rotate<4>(sum);
     sum += row_rotate<2>(sum);
     sum += row_rotate<1>(sum);
     const int from = lane / LH * 16;
     f32x4 A = {0.f, 0.f, 0.f, 0.f};
-    auto fold = [&](auto n) {
+    auto fold = [&](auto n, float weight) {
 #pragma unroll
       for (int i = 0; i < decltype(n)::value; ++i) {
-        const float wi = __shfl(w, from + i);   // 0 past the splits
+        const float wi = __shfl(weight, from + i);   // 0 past the splits
 #pragma unroll
         for (int e = 0; e < 4; ++e) A[e] = fmaf(wi, a[i][e], A[e]);
       }
     };
-    if (nsp <= 4) fold(std::integral_constant<int, 4>{});
-    else fold(std::integral_constant<int, kMaxSplits>{});
+    if (nsp <= 4) fold(std::integral_constant<int, 4>{}, w[0]);
+    else fold(std::integral_constant<int, kMaxSplits>{}, w[0]);
+#pragma unroll
+    for (int c = 1; c < ROUNDS; ++c)
+      if (c * kMaxSplits < nsp) {
+        load(std::integral_constant<int, kMaxSplits>{}, c * kMaxSplits);
+        fold(std::integral_constant<int, kMaxSplits>{}, w[c]);
+      }
     const float L = __shfl(sum, from);
     if (SCORED && sp == 0 && lane / 16 < kWave / LH && wave * (kWave / LH) + lane / 16 < G)
       rows.lse[static_cast<size_t>(b) * Hq + kvh * G + head] = top + __builtin_amdgcn_logf(sum);
@@ -452,8 +482,6 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
       bool vis = r < r_end;
       if (MASKED) vis = vis && (r >= len || ((roles >> (8 * i)) & 0xFF) != kText);
       x[i] = vis ? sacc[i] * scale_log2 : -INFINITY;
-      // the rounded product is what is kept and what the exponential takes: the same with and without weights
-      if constexpr (Q4 || SCORED) asm("" : "+v"(x[i]));
       mloc = fmaxf(mloc, x[i]);
     }
     if constexpr (SCORED) {   // one store a group, which the waits of the pipeline count
@@ -613,97 +641,178 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
       *reinterpret_cast<u32x4 *>((lane < DC ? kbase : vbase) + dst) = *reinterpret_cast<const u32x4 *>(&app_lds[lane * 8]);
     }
   } else {
-    // 4-bit rows: no ring, since a group is only a kilobyte of codes per tensor and fits in the registers.  Lane
-    // (col, quarter) loads a quarter of row col: D / 4 values, one block (D = 128) or half of one.  That quarter
-    // is its part of the score product's depth (Q^T is laid out alike), K goes from the codes to the operand
-    // without leaving the lane, and V through the wave's LDS for the transposing reads.
-    constexpr int DL = D / 4;        // values of a lane
-    constexpr int CW = DL / 8;       // ... in words of eight codes
+    // 4-bit rows, 32 at a time.  A block of rows is two kilobytes of codes per tensor and stays in registers: K of the
+    // next block is loaded once this one's scores are taken, V once this one's is on its way through LDS, where it
+    // goes as bf16 for the transposing reads.
+    //
+    // Scores: lane (col, quarter) takes a quarter of row col, D / 4 values, as its part of the depth (q is laid out
+    // alike) and decodes it into the operand.  (v_mfma_scale_f32_16x16x128_f8f6f4 would take the codes and scales as
+    // they are, but aligns a block's products to the largest and drops what lies more than 13 bits below it; with q
+    // in two e4m3 parts scores were off by 1e-5 of their products' sum.)
+    // Columns col and col + 8 are the same q-head's.
+    //
+    // Values: columns 0 .. 7 carry the bf16 rounding of the probabilities, columns 8 .. 15 what it left, so one
+    // product of depth 32 takes 32 rows of V; the two columns of a head are added at the end.
+    constexpr int BR = 32;                    // rows of a block
+    constexpr int LV = D / kQ4Block;          // lanes that hold a row of V, a quantisation block each
+    constexpr int NV = BR * LV / kWave;       // ... and loads of a block's V
+    constexpr int CW = D / 32;                // words of a lane's K codes, eight each
     typedef uint32_t codes_t __attribute__((ext_vector_type(CW)));
-    struct Raw { codes_t k, v; uint32_t ks, vs; };
-    const size_t lane_codes = (static_cast<size_t>(base) * Hkv + kvh) * (D / 2) + quarter * (DL / 2);
-    const size_t lane_scale = (static_cast<size_t>(base) * Hkv + kvh) * (D / kQ4Block) + quarter * DL / kQ4Block;
-    uint8_t *const kcode = reinterpret_cast<uint8_t *>(kc) + lane_codes, *const vcode = reinterpret_cast<uint8_t *>(vc) + lane_codes;
-    uint8_t *const kscale = rows.ks + lane_scale, *const vscale = rows.vs + lane_scale;
-    auto fetch = [&](int g) {   // rows past len load row len, which the request owns
-      const size_t r = min(r_begin + kGroupRows * g + col, len);
-      Raw x;
-      x.k = *reinterpret_cast<const codes_t *>(kcode + r * (Hkv * (D / 2)));
-      x.v = *reinterpret_cast<const codes_t *>(vcode + r * (Hkv * (D / 2)));
-      x.ks = kscale[r * (Hkv * (D / kQ4Block))];
-      x.vs = vscale[r * (Hkv * (D / kQ4Block))];
+    typedef SONIC_GLOBAL uint8_t *plane_t;
+    const int row_codes = Hkv * (D / 2), row_scales = Hkv * (D / kQ4Block);
+    auto plane = [&](void *p, int row) {
+      const char *at = static_cast<char *>(p) + static_cast<size_t>(base) * row + kvh * (row / Hkv);
+      return (plane_t)(const_cast<char *>(uniform_ptr(at)));
+    };
+    const plane_t kcode = plane(kc, row_codes), vcode = plane(vc, row_codes);
+    const plane_t kscale = plane(rows.ks, row_scales), vscale = plane(rows.vs, row_scales);
+    const int k_blk = quarter * LV / 4, v_blk = lane % LV, v_row = lane / LV;
+    // A block's codes and scales (bytes: widened where they are used, not where they are loaded).  Rows past len
+    // load row len, which the request owns.
+    struct KRaw { codes_t c[2]; uint8_t s[2]; };
+    struct VRaw { u32x4 c[NV]; uint8_t s[NV]; };
+    auto fetch_k = [&](int n) {
+      const int r0 = r_begin + BR * n;
+      KRaw x;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const size_t r = min(r0 + 16 * t + col, len);
+        x.c[t] = *(const SONIC_GLOBAL codes_t *)(kcode + r * row_codes + 4 * CW * quarter);
+        x.s[t] = kscale[r * row_scales + k_blk];
+      }
       return x;
     };
-    // the new token's row, in registers: every wave rounds its k and v alike, the one whose group it is
-    // in takes it from there and appends it
-    const bool owner = ngroups > 0 && r_end == n_ctx && (ngroups - 1) % NW == wave;
-    auto round_row = [&](const uint16_t *src, codes_t *codes, uint32_t *byte) {
-      uint32_t w[DL / 2];
+    auto fetch_v = [&](int n) {
+      const int r0 = r_begin + BR * n;
+      VRaw x;
 #pragma unroll
-      for (int i = 0; i < DL / 8; ++i) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(src + quarter * DL + 8 * i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
+      for (int t = 0; t < NV; ++t) {
+        const size_t r = min(r0 + kWave / LV * t + v_row, len);
+        x.c[t] = *(const SONIC_GLOBAL u32x4 *)(vcode + r * row_codes + 16 * v_blk);
+        x.s[t] = vscale[r * row_scales + v_blk];
       }
-      uint32_t top = q4_top(w);
-      if (DL < kQ4Block) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16)));
-      *byte = q4_scale_byte(top);
-#pragma unroll
-      for (int i = 0; i < CW; ++i) (*codes)[i] = q4_encode8(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3], *byte);
+      return x;
     };
-    constexpr int P = 4;   // groups in flight
-    Raw raw[P], fresh_row;
+    const int nblocks = stop ? 0 : (r_end - r_begin + BR - 1) / BR;
+    // The new token's row: the wave whose last block it is in rounds k and v, appends the row, and takes it from LDS
+    // where that block is processed.
+    const bool owner = nblocks > 0 && r_end == n_ctx && (nblocks - 1) % NW == wave;
+    __shared__ u32x4 new_codes[2][LV];
+    __shared__ uint8_t new_scales[2][LV];
+    KRaw k_raw;
+    VRaw v_raw;
     if (!stop) {
-      const uint16_t *q0 = q + (static_cast<size_t>(b) * Hq + kvh * G + (col < G ? col : 0)) * D + quarter * DL;
+      const uint16_t *q0 = q + (static_cast<size_t>(b) * Hq + kvh * G + ((col & 7) < G ? (col & 7) : 0)) * D + quarter * (D / 4);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(q0 + 8 * ks);
+      k_raw = fetch_k(wave);
+      v_raw = fetch_v(wave);
+      if (owner && lane < 2 * LV) {
+        const int blk = lane % LV;
+        const bool is_v = lane >= LV;
+        const uint16_t *src = (is_v ? vnew : knew) + kQ4Block * blk;
+        uint32_t w[16];
 #pragma unroll
-      for (int p = 0; p < P; ++p) raw[p] = fetch(wave + p * NW);
-      if (owner) {
-        round_row(knew, &fresh_row.k, &fresh_row.ks);
-        round_row(vnew, &fresh_row.v, &fresh_row.vs);
-        if (col == 0) {
-          *reinterpret_cast<codes_t *>(kcode + static_cast<size_t>(len) * (Hkv * (D / 2))) = fresh_row.k;
-          *reinterpret_cast<codes_t *>(vcode + static_cast<size_t>(len) * (Hkv * (D / 2))) = fresh_row.v;
-          if (quarter * DL % kQ4Block == 0) {
-            kscale[static_cast<size_t>(len) * (Hkv * (D / kQ4Block))] = fresh_row.ks;
-            vscale[static_cast<size_t>(len) * (Hkv * (D / kQ4Block))] = fresh_row.vs;
+        for (int i = 0; i < 4; ++i) {
+          const u32x4 x = *reinterpret_cast<const u32x4 *>(src + 8 * i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
+        }
+        const uint32_t byte = q4_scale_byte(q4_top(w));
+        u32x4 codes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes[i] = q4_encode8(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3], byte);
+        new_codes[is_v][blk] = codes;
+        new_scales[is_v][blk] = static_cast<uint8_t>(byte);
+        *(SONIC_GLOBAL u32x4 *)((is_v ? vcode : kcode) + static_cast<size_t>(len) * row_codes + 16 * blk) = codes;
+        (is_v ? vscale : kscale)[static_cast<size_t>(len) * row_scales + blk] = static_cast<uint8_t>(byte);
+      }
+    }
+    const float first_part = col >= 8 ? 1.f : 0.f;   // what a probability's second value leaves out: its first
+    uint16_t *const vtile = ring + wave * RING;   // [32 rows][D], 32-byte segments swizzled like the ring's
+    for (int n = wave; n < nblocks; n += NW) {
+      const int r0 = r_begin + BR * n;
+      const bool tail = r0 + BR >= r_end;   // the split's last block
+      if (tail) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (owner && r0 + 16 * t + col == len) {
+            k_raw.c[t] = *reinterpret_cast<const codes_t *>(reinterpret_cast<const uint8_t *>(&new_codes[0][0]) + 4 * CW * quarter);
+            k_raw.s[t] = new_scales[0][k_blk];
           }
         }
-      }
-    }
-    uint16_t *const vtile = ring + wave * SLOT;   // [16 rows][D], 32-byte segments swizzled like the ring's
-    auto process = [&](int g, Raw x) {
-      const int r0 = r_begin + kGroupRows * g;
-      if (r0 + kGroupRows >= r_end) {   // the last group
-        if (owner && r0 + col == len) x = fresh_row;
-        if (r0 + col >= r_end) {   // past the split: zeros (a NaN there would stay one under its weight of zero)
-          x.k = x.v = codes_t(0);
-          x.ks = x.vs = 0;
+#pragma unroll
+        for (int t = 0; t < NV; ++t) {
+          const int r = r0 + kWave / LV * t + v_row;
+          if (owner && r == len) v_raw.c[t] = new_codes[1][v_blk], v_raw.s[t] = new_scales[1][v_blk];
+          if (r >= r_end) v_raw.c[t] = u32x4{0, 0, 0, 0}, v_raw.s[t] = 0;   // (a NaN would stay one under its weight of zero)
         }
       }
-      const float vs = q4_scale(x.vs), ks_ = q4_scale(x.ks);
+      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-      for (int i = 0; i < CW; ++i) {
-        const int seg = (quarter * DL + 8 * i) / 16;
-        *reinterpret_cast<bf16x8 *>(vtile + col * D + (seg ^ (col & VSWZ)) * 16 + (i & 1) * 8) = q4_decode8(x.v[i], vs);
+      for (int t = 0; t < 2; ++t) {
+        const float scale = q4_scale(k_raw.s[t]);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q4_decode8(k_raw.c[t][ks], scale), qf[ks], s[t], 0, 0, 0);
       }
-      f32x4 sacc = {0.f, 0.f, 0.f, 0.f};
+      k_raw = fetch_k(n + NW);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) sacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q4_decode8(x.k[ks], ks_), qf[ks], sacc, 0, 0, 0);
-      const bf16x8 pp = soften(sacc, r0, 0);
-      add_values(vtile, pp);
-    };
-    for (int g = wave; g < ngroups; g += P * NW) {
+      for (int t = 0; t < NV; ++t) {
+        const float vs = q4_scale(v_raw.s[t]);
+        const int r = kWave / LV * t + v_row;
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        if (g + p * NW < ngroups) {
-          const Raw x = raw[p];
-          raw[p] = fetch(g + (p + P) * NW);
-          process(g + p * NW, x);
-        }
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<bf16x8 *>(vtile + r * D + ((2 * v_blk + i / 2) ^ (r & VSWZ)) * 16 + (i & 1) * 8) = q4_decode8(v_raw.c[t][i], vs);
+      }
+      v_raw = fetch_v(n + NW);
+      // lane (col, quarter): rows r0 + 16 t + 4 quarter + i of column col
+      if (tail) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][i] = r0 + 16 * t + 4 * quarter + i < r_end ? s[t][i] : -INFINITY;
+      }
+      if constexpr (SCORED) {
+        if (col < G)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)   // (a row's scores have room up to a multiple of 16)
+            if (r0 + 16 * t < r_end) *reinterpret_cast<f32x4 *>(score_row + r0 + 16 * t) = s[t] * scale_log2;
+      }
+      float mloc = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      mloc = pair32_max(pair16_max(mloc)) * scale_log2;
+      if (__any(mloc > m_run + 8.f)) {   // rescale only when the max grows by more than 2^8
+        const float m_new = fmaxf(m_run, mloc);
+        const float corr = (m_run == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        l_run *= corr;
+#pragma unroll
+        for (int i = 0; i < DB; ++i) oacc[i] *= corr;
+      }
+      f32x8 p;   // (a masked score is -infinity, and every block has a row that is not)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], scale_log2, -m_run));
+      const f32x8 first = __builtin_convertvector(__builtin_convertvector(p, bf16x8), f32x8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = fmaf(-first_part, first[i], p[i]);
+      const bf16x8 pp = __builtin_convertvector(p, bf16x8);
+      const bf16x8 one[1] = {pp};
+      l_run += rounded_sum(one);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const uint16_t *pa = vtile + tr_off + ((db ^ tr_swz) * 16);
+        // C-style cast: the transposing read takes an LDS-qualified pointer
+        const v4i16 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)pa);
+        const v4i16 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(pa + 16 * D));
+        const bf16x8 aa = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+        oacc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aa, pp, oacc[db], 0, 0, 0);
       }
     }
+    // the two columns of a head
+    l_run += row_rotate<8>(l_run);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) oacc[db][e] += row_rotate<8>(oacc[db][e]);
   }
 
   // ---- merge: columns across the four quarters, then the waves through LDS ----
@@ -769,7 +878,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void decode_kernel(
 template <int D, int G, bool MASKED, int NW, bool BAL, bool Q4, bool SCORED>
 static void launch_decode_variant(int batch, int Hkv, int max_ctx, const DecodeShape &sh, const DecodeCall &c, const DecodeRows &rows,
                                   DecodeWs ws, hipStream_t stream) {
-  const dim3 grid = BAL && row_bytes<D, Q4>(Hkv) >= kLongRow ? dim3(Hkv, sh.splits) : dim3(sh.splits, Hkv, BAL ? 1 : batch);
+  const long units = static_cast<long>(sh.splits) * (BAL ? 1 : batch);   // (see the kernel)
+  const dim3 grid = Q4 ? dim3((units + kNumXcd - 1) / kNumXcd * kNumXcd * Hkv)
+                       : BAL && Hkv * D * 2 >= kLongRow ? dim3(Hkv, sh.splits) : dim3(sh.splits, Hkv, BAL ? 1 : batch);
   decode_kernel<D, G, MASKED, NW, BAL, Q4, SCORED><<<grid, dim3(NW * kWave), 0, stream>>>(
       c.kc, c.vc, c.row_off, c.row_cap, c.cache_len, c.row_role, c.q, c.k_new, c.v_new, c.out, ws, rows, c.status, Hkv, sh.splits,
       max_ctx, batch, sh.target, c.scale_log2);
