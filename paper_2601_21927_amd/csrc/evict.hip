@@ -18,7 +18,7 @@
 namespace sonic {
 
 constexpr int kSelectThreads = 1024;
-constexpr int kSelectRows = 4;                              // consecutive rows of a thread
+constexpr int kSelectRows = 8;                              // consecutive rows of a thread
 constexpr int kSelectChunk = kSelectThreads * kSelectRows;
 constexpr int kMoveThreads = 256;
 constexpr int kMoveUnroll = 4;
@@ -45,85 +45,136 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
+// The digit of the radix search's pass at `shift`, counted from above: writes the digit that holds the `need`-th key, how
+// many of its keys are wanted, and how many it has.  kCopies histograms (a lane has its own: weights share their
+// exponents, and 64 lanes adding to one word take turns) are added up first.
+constexpr int kCopies = 16, kCopyStride = 257;
+struct Digit {
+  int digit, rest, count;
+};
+__device__ __forceinline__ void find_digit(const int *copies, int *hist, int need, Digit *found) {
+  if (threadIdx.x < 256) {
+    int sum = 0;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) sum += copies[c * kCopyStride + threadIdx.x];
+    hist[threadIdx.x] = sum;
+  }
+  __syncthreads();
+  if (threadIdx.x < kWave) {
+    // lane l holds digits 255 - 4 l down to 252 - 4 l
+    int h[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += h[i] = hist[255 - 4 * threadIdx.x - i];
+    int above = wave_scan(sum) - sum;
+    if (above < need && above + sum >= need) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (above < need && above + h[i] >= need) *found = Digit{static_cast<int>(255 - 4 * threadIdx.x - i), need - above, h[i]};
+        above += h[i];
+      }
+    }
+  }
+  __syncthreads();
+}
+
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, EvictWs ws) {
   __shared__ int lds[2 * (kSelectThreads / kWave)];
+  __shared__ int copies[kCopies * kCopyStride];
   __shared__ int hist[256];
-  __shared__ int s_ok, s_digit, s_rest, s_first;
+  __shared__ int s_ok, s_first;
+  __shared__ Digit s_digit;
   const int b = blockIdx.x;
   // workgroup 0's look at the status word decides for the whole call
   const bool clear = b != 0 || block_status_clear(c.status, &s_ok);
   EvictReq own;
   const int own_code = evict_check(b, c, &own);
+  const float *w = c.row_weight + c.row_off[b];
+  const int lo = own.head, hi = own.len - own.tail;
+  // A thread has kSelectRows consecutive rows of a chunk; the first chunk's keys stay in registers.  Head and tail
+  // rows are as if heavier than any, rows past the end as if lighter: no weight has their keys.
+  const int mine = kSelectRows * threadIdx.x;
+  auto load_keys = [&](int base, uint32_t (&key)[kSelectRows]) {
+    float x[kSelectRows];
+#pragma unroll
+    for (int i = 0; i < kSelectRows; ++i) {
+      const int r = base + mine + i;
+      x[i] = r >= lo && r < hi ? w[r] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kSelectRows; ++i) {
+      const int r = base + mine + i;
+      key[i] = r >= own.len ? 0u : r < lo || r >= hi ? 0xFFFFFFFFu : weight_key(x[i]);
+    }
+  };
+  uint32_t first_keys[kSelectRows];
+  load_keys(0, first_keys);
   int bad = 0;
   for (int j = threadIdx.x; j < c.batch; j += kSelectThreads) {
     EvictReq r;
     bad |= evict_check(j, c, &r) != 0;
   }
+  for (int i = threadIdx.x; i < kCopies * kCopyStride; i += kSelectThreads) copies[i] = 0;
+  if (threadIdx.x == 0) s_first = own.kept;
   bad = __syncthreads_or(bad);
   if (own_code != 0 && threadIdx.x == 0) raise_status(c.status, own_code);
   if (b == 0 && threadIdx.x == 0) ws.ctrl[0] = clear && !bad;
   if (bad || !clear) return;
 
-  const float *w = c.row_weight + c.row_off[b];
   int32_t *list = ws.list + static_cast<size_t>(b) * c.max_rows;
-  const int lo = own.head, hi = own.len - own.tail;
-  int take = own.kept - own.head - own.tail;   // of the middle rows
-  // the key of the lightest kept row (threshold), and how many of the rows at it are kept (rest)
-  uint32_t threshold = 0;
+  const int take = own.kept - own.head - own.tail;   // of the middle rows
+  // kept are the keys above the threshold, and the first `rest` of those at it
+  uint32_t threshold = 0;   // all: every key is above 0
   int rest = 0;
-  if (take == hi - lo) {
-    threshold = 0, rest = 0;   // all: every key is above 0 (only negative NaN patterns map to 0, and those are -infinity)
-  } else if (take == 0) {
-    threshold = 0xFFFFFFFFu;
-  } else {
+  if (take < hi - lo) {
+    threshold = 0xFFFFFFFEu;   // none: only head and tail are above
     int need = take;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = threadIdx.x; i < 256; i += kSelectThreads) hist[i] = 0;
-      __syncthreads();
-      for (int r = lo + threadIdx.x; r < hi; r += kSelectThreads) {
-        const uint32_t key = weight_key(w[r]);
-        if (shift == 24 || (key >> (shift + 8)) == (threshold >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255], 1);
-      }
-      __syncthreads();
-      if (threadIdx.x < kWave) {
-        // lane l holds digits 255 - 4 l down to 252 - 4 l: the digit where the count from above reaches `need`
-        int h[4], sum = 0;
+    uint32_t prefix = 0;
+    for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
+      int *const copy = copies + (threadIdx.x % kCopies) * kCopyStride;
+      for (int base = 0; base < hi; base += kSelectChunk) {
+        uint32_t key[kSelectRows];
+        if (base == 0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += h[i] = hist[255 - 4 * threadIdx.x - i];
-        int above = wave_scan(sum) - sum;
-        if (above < need && above + sum >= need) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (above < need && above + h[i] >= need) {
-              s_digit = 255 - 4 * threadIdx.x - i;
-              s_rest = need - above;
-            }
-            above += h[i];
-          }
+          for (int i = 0; i < kSelectRows; ++i) key[i] = first_keys[i];
+        } else {
+          load_keys(base, key);
         }
+#pragma unroll
+        for (int i = 0; i < kSelectRows; ++i)
+          if (key[i] - 1u < 0xFFFFFFFEu && (shift == 24 || (key[i] >> (shift + 8)) == prefix))
+            atomicAdd(&copy[(key[i] >> shift) & 255], 1);
       }
       __syncthreads();
-      threshold |= static_cast<uint32_t>(s_digit) << shift;
-      need = s_rest;
+      find_digit(copies, hist, need, &s_digit);
+      const Digit d = s_digit;
+      prefix = prefix << 8 | static_cast<uint32_t>(d.digit);
+      threshold = prefix << shift;
+      rest = need = d.rest;
+      if (d.rest == d.count) {   // all of the digit's keys are kept: no need to tell them apart
+        threshold -= 1;          // (not below 0: a key is above 0)
+        rest = need = 0;
+      } else if (shift > 0) {
+        for (int i = threadIdx.x; i < kCopies * kCopyStride; i += kSelectThreads) copies[i] = 0;
+        __syncthreads();
+      }
     }
-    rest = need;
   }
 
   // the list, in row order
-  if (threadIdx.x == 0) s_first = own.kept;
-  __syncthreads();
   int listed = 0, equal = 0;
   for (int base = 0; base < own.len; base += kSelectChunk) {
-    const int r0 = base + kSelectRows * threadIdx.x;
     uint32_t key[kSelectRows];
+    if (base == 0) {
+#pragma unroll
+      for (int i = 0; i < kSelectRows; ++i) key[i] = first_keys[i];
+    } else {
+      load_keys(base, key);
+    }
     int sure = 0, ties = 0;
 #pragma unroll
     for (int i = 0; i < kSelectRows; ++i) {
-      const int r = r0 + i;
-      // past the end: as if dropped; head and tail: as if heavier than any
-      key[i] = r >= own.len ? 0u : r < lo || r >= hi ? 0xFFFFFFFFu : weight_key(w[r]);
-      sure += r < own.len && (r < lo || r >= hi || key[i] > threshold);
-      ties += r >= lo && r < hi && key[i] == threshold;
+      sure += key[i] > threshold;
+      ties += rest > 0 && key[i] == threshold;
     }
     // a tie is kept while fewer than `rest` come before it
     const int x[2] = {sure, ties};
@@ -133,13 +184,13 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, Evi
     int at = listed + below[0] + min(tie_rank, rest) - min(equal, rest);
 #pragma unroll
     for (int i = 0; i < kSelectRows; ++i) {
-      const int r = r0 + i;
-      if (r >= own.len) break;
-      const bool mid = r >= lo && r < hi;
-      const bool tie = mid && key[i] == threshold;
-      if (!mid || key[i] > threshold || (tie && tie_rank < rest)) list[at++] = r;
-      else if (at == r) s_first = r;   // the first dropped row: those before it stay where they are
-      tie_rank += tie;
+      const int r = base + mine + i;
+      if (r < own.len) {
+        const bool tie = rest > 0 && key[i] == threshold;
+        if (key[i] > threshold || (tie && tie_rank < rest)) list[at++] = r;
+        else if (at == r) s_first = r;   // the first dropped row: those before it stay where they are
+        tie_rank += tie;
+      }
     }
     listed += total[0] + min(equal + total[1], rest) - min(equal, rest);
     equal += total[1];

@@ -333,66 +333,83 @@ def nexus_recon_targets(cu_seqlens, role, turn_id, h, target, cos_target, entrop
 
 
 # ----------------------------------------------------------------- 4-bit rows
-def _on_one_device(*ts):
-    """The device of the call's tensors: a call with tensors of two GPUs is refused, and one whose tensors are not
-    on the current GPU is made on theirs."""
-    _dev(*ts)
-    devs = {t.device for t in ts if t is not None}
-    if len(devs) != 1:
-        raise ValueError("tensors of one call must be on one GPU")
-    return torch.cuda.device(devs.pop())
-
-
-def _shapes(where, **named):
-    """named=(tensor, shape): a None in a shape stands for any size."""
-    for name, (t, shape) in named.items():
-        if t is not None and (t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape))):
+def _pass(where, fn, stream, head, tensors, tail=()):
+    """Call fn(*head, pointers, *tail, stream) for tensors = [(name, tensor, dtype, shape or None)], or a number in a
+    tensor's place, once every tensor is contiguous, of its type and shape, and on one GPU.  The call is made on that
+    GPU, on its current stream unless one is given."""
+    dev, args = None, list(head)
+    for name, t, dtype, shape in tensors:
+        if t is None or dtype is None:
+            args.append(t)
+            continue
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if shape is not None and t.shape != shape:
             raise ValueError(f"{where}: {name} must be {shape}, got {tuple(t.shape)}")
+        if not t.is_contiguous():
+            raise ValueError("tensors passed to libsonic must be contiguous")
+        d = t.get_device()
+        if d != dev:
+            if d < 0:
+                raise ValueError("libsonic GPU entry points take device tensors")
+            if dev is not None:
+                raise ValueError("tensors of one call must be on one GPU")
+            dev = d
+        args.append(t.data_ptr())
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif stream.device_index != dev:
+        raise ValueError("the stream must be one of the tensors' GPU")
+    args += tail
+    args.append(stream.cuda_stream)
+    if dev == torch.cuda.current_device():
+        return fn(*args)
+    with torch.cuda.device(dev):
+        return fn(*args)
 
 
-def _q4_rows(where, Hkv, d, k_cache, k_scale, v_cache, v_scale):
-    _types(k_cache=(k_cache, _U8), k_scale=(k_scale, _U8), v_cache=(v_cache, _U8), v_scale=(v_scale, _U8))
-    rows = k_cache.shape[0]
-    _shapes(where, k_cache=(k_cache, (rows, Hkv, d // 2)), v_cache=(v_cache, (rows, Hkv, d // 2)),
-            k_scale=(k_scale, (rows, Hkv, d // 32)), v_scale=(v_scale, (rows, Hkv, d // 32)))
+def _number(x):
+    """A plain argument between the tensors of _pass."""
+    return ("", x, None, None)
+
+
+def _q4_planes(rows, Hkv, d, k_cache, k_scale, v_cache, v_scale):
+    return [("k_cache", k_cache, _U8, (rows, Hkv, d // 2)), ("k_scale", k_scale, _U8, (rows, Hkv, d // 32)),
+            ("v_cache", v_cache, _U8, (rows, Hkv, d // 2)), ("v_scale", v_scale, _U8, (rows, Hkv, d // 32))]
 
 
 def kv_compact_q4(cu_seqlens, role, k, v, k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, cache_len, keep_idx,
                   dev_status, max_seqlen: int, stream=None) -> int:
     """kv_compact into 4-bit rows: k_cache/v_cache uint8 [rows,Hkv,d/2] codes, k_scale/v_scale uint8 [rows,Hkv,d/32]."""
-    with _on_one_device(cu_seqlens, role, k, v, k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, cache_len, keep_idx,
-                        dev_status):
-        T, Hkv, d = k.shape
-        B = cu_seqlens.numel() - 1
-        _q4_rows("kv_compact_q4", Hkv, d, k_cache, k_scale, v_cache, v_scale)
-        _types(cu_seqlens=(cu_seqlens, _I32), role=(role, _U8), k=(k, _BF16), v=(v, _BF16), cache_row_off=(cache_row_off, _I64),
-               cache_row_cap=(cache_row_cap, _I32), cache_len=(cache_len, _I32), keep_idx=(keep_idx, _I32),
-               dev_status=(dev_status, _I32))
-        _shapes("kv_compact_q4", role=(role, (T,)), v=(v, (T, Hkv, d)), cache_row_off=(cache_row_off, (B,)),
-                cache_row_cap=(cache_row_cap, (B,)), cache_len=(cache_len, (B,)), keep_idx=(keep_idx, (k_cache.shape[0],)))
-        return int(lib().sonic_kv_compact_q4(
-            B, T, int(max_seqlen), Hkv, d, _ptr(cu_seqlens), _ptr(role), _ptr(k), _ptr(v), _ptr(k_cache), _ptr(k_scale), _ptr(v_cache),
-            _ptr(v_scale), _ptr(cache_row_off), _ptr(cache_row_cap), _ptr(cache_len), _ptr(keep_idx), _ptr(dev_status),
-            _stream(stream)))
+    T, Hkv, d = k.shape
+    B, rows = cu_seqlens.numel() - 1, k_cache.shape[0]
+    return _pass("kv_compact_q4", lib().sonic_kv_compact_q4, stream, (B, T, int(max_seqlen), Hkv, d), [
+        ("cu_seqlens", cu_seqlens, _I32, None), ("role", role, _U8, (T,)), ("k", k, _BF16, None), ("v", v, _BF16, (T, Hkv, d)),
+        *_q4_planes(rows, Hkv, d, k_cache, k_scale, v_cache, v_scale), ("cache_row_off", cache_row_off, _I64, (B,)),
+        ("cache_row_cap", cache_row_cap, _I32, (B,)), ("cache_len", cache_len, _I32, (B,)), ("keep_idx", keep_idx, _I32, (rows,)),
+        ("dev_status", dev_status, _I32, None)])
 
 
 def cache_expand_q4(k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, row_begin, row_end, k, v, out_row_off,
                     out_row_cap, dev_status, max_rows: int, stream=None) -> int:
     """4-bit rows row_begin[b] .. row_end[b] of every request to rows out_row_off[b] .. of k/v [n,Hkv,d] bf16."""
-    with _on_one_device(k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, row_begin, row_end, k, v, out_row_off,
-                        out_row_cap, dev_status):
-        _, Hkv, d = k.shape
-        B = cache_row_off.numel()
-        _q4_rows("cache_expand_q4", Hkv, d, k_cache, k_scale, v_cache, v_scale)
-        _types(cache_row_off=(cache_row_off, _I64), cache_row_cap=(cache_row_cap, _I32), row_begin=(row_begin, _I32),
-               row_end=(row_end, _I32), k=(k, _BF16), v=(v, _BF16), out_row_off=(out_row_off, _I64),
-               out_row_cap=(out_row_cap, _I32), dev_status=(dev_status, _I32))
-        _shapes("cache_expand_q4", v=(v, tuple(k.shape)), cache_row_cap=(cache_row_cap, (B,)), row_begin=(row_begin, (B,)),
-                row_end=(row_end, (B,)), out_row_off=(out_row_off, (B,)), out_row_cap=(out_row_cap, (B,)))
-        return int(lib().sonic_cache_expand_q4(
-            B, int(max_rows), Hkv, d, _ptr(k_cache), _ptr(k_scale), _ptr(v_cache), _ptr(v_scale), _ptr(cache_row_off),
-            _ptr(cache_row_cap), _ptr(row_begin), _ptr(row_end), _ptr(k), _ptr(v), _ptr(out_row_off), _ptr(out_row_cap),
-            _ptr(dev_status), _stream(stream)))
+    n, Hkv, d = k.shape
+    B = cache_row_off.numel()
+    return _pass("cache_expand_q4", lib().sonic_cache_expand_q4, stream, (B, int(max_rows), Hkv, d), [
+        *_q4_planes(k_cache.shape[0], Hkv, d, k_cache, k_scale, v_cache, v_scale), ("cache_row_off", cache_row_off, _I64, None),
+        ("cache_row_cap", cache_row_cap, _I32, (B,)), ("row_begin", row_begin, _I32, (B,)), ("row_end", row_end, _I32, (B,)),
+        ("k", k, _BF16, None), ("v", v, _BF16, (n, Hkv, d)), ("out_row_off", out_row_off, _I64, (B,)),
+        ("out_row_cap", out_row_cap, _I32, (B,)), ("dev_status", dev_status, _I32, None)])
+
+
+def _decode_tensors(planes, B, Hq, Hkv, d, rows, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, softmax_scale, out,
+                    row_weight, workspace):
+    scale = 0.0 if softmax_scale is None else float(softmax_scale)   # 0: the library's 1/sqrt(d)
+    return [*planes, ("cache_row_off", cache_row_off, _I64, (B,)), ("cache_row_cap", cache_row_cap, _I32, (B,)),
+            ("cache_len", cache_len, _I32, (B,)), ("q", q, _BF16, None), ("k_new", k_new, _BF16, (B, Hkv, d)),
+            ("v_new", v_new, _BF16, (B, Hkv, d)), _number(scale), ("out", out, _F32, (B, Hq, d)),
+            ("row_weight", row_weight, _F32, (rows,)), ("workspace", workspace, workspace.dtype, None),
+            _number(workspace.numel() * workspace.element_size())]
 
 
 def decode_q4_workspace_bytes(batch: int, num_q_heads: int, head_dim: int, max_ctx: int, weighted: bool) -> int:
@@ -402,25 +419,12 @@ def decode_q4_workspace_bytes(batch: int, num_q_heads: int, head_dim: int, max_c
 def compressed_decode_q4(k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, workspace,
                          dev_status, max_ctx: int, row_weight=None, softmax_scale=None, stream=None) -> int:
     """compressed_decode over 4-bit rows; row_weight fp32 [rows] or None: each row's attention is added to it."""
-    with _on_one_device(k_cache, k_scale, v_cache, v_scale, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, workspace,
-                        dev_status, row_weight):
-        B, Hq, d = q.shape
-        Hkv = k_new.shape[1]
-        _q4_rows("compressed_decode_q4", Hkv, d, k_cache, k_scale, v_cache, v_scale)
-        _decode_args("compressed_decode_q4", B, Hq, Hkv, d, k_cache.shape[0], cache_row_off, cache_row_cap, cache_len, q, k_new, v_new,
-                     out, dev_status, row_weight)
-        scale = 0.0 if softmax_scale is None else float(softmax_scale)   # 0: the library's 1/sqrt(d)
-        return int(lib().sonic_compressed_decode_q4(
-            B, Hq, Hkv, d, int(max_ctx), _ptr(k_cache), _ptr(k_scale), _ptr(v_cache), _ptr(v_scale), _ptr(cache_row_off),
-            _ptr(cache_row_cap), _ptr(cache_len), _ptr(q), _ptr(k_new), _ptr(v_new), scale, _ptr(out), _ptr(row_weight),
-            _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream)))
-
-
-def _decode_args(where, B, Hq, Hkv, d, rows, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, dev_status, row_weight):
-    _types(cache_row_off=(cache_row_off, _I64), cache_row_cap=(cache_row_cap, _I32), cache_len=(cache_len, _I32), q=(q, _BF16),
-           k_new=(k_new, _BF16), v_new=(v_new, _BF16), out=(out, _F32), dev_status=(dev_status, _I32), row_weight=(row_weight, _F32))
-    _shapes(where, k_new=(k_new, (B, Hkv, d)), v_new=(v_new, (B, Hkv, d)), out=(out, (B, Hq, d)), cache_row_off=(cache_row_off, (B,)),
-            cache_row_cap=(cache_row_cap, (B,)), cache_len=(cache_len, (B,)), row_weight=(row_weight, (rows,)))
+    B, Hq, d = q.shape
+    Hkv, rows = k_new.shape[1], k_cache.shape[0]
+    return _pass("compressed_decode_q4", lib().sonic_compressed_decode_q4, stream, (B, Hq, Hkv, d, int(max_ctx)), [
+        *_decode_tensors(_q4_planes(rows, Hkv, d, k_cache, k_scale, v_cache, v_scale), B, Hq, Hkv, d, rows, cache_row_off,
+                         cache_row_cap, cache_len, q, k_new, v_new, softmax_scale, out, row_weight, workspace),
+        ("dev_status", dev_status, _I32, None)])
 
 
 # ----------------------------------------------------------------- row weights, eviction
@@ -431,34 +435,22 @@ def decode_weighted_workspace_bytes(batch: int, num_q_heads: int, head_dim: int,
 def compressed_decode_weighted(k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, row_weight, workspace,
                                dev_status, max_ctx: int, softmax_scale=None, stream=None) -> int:
     """compressed_decode that also adds each row's attention, averaged over the q-heads, to row_weight fp32 [rows]."""
-    with _on_one_device(k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out, row_weight, workspace,
-                        dev_status):
-        B, Hq, d = q.shape
-        Hkv = k_new.shape[1]
-        rows = k_cache.shape[0]
-        _types(k_cache=(k_cache, _BF16), v_cache=(v_cache, _BF16))
-        _shapes("compressed_decode_weighted", k_cache=(k_cache, (rows, Hkv, d)), v_cache=(v_cache, (rows, Hkv, d)))
-        _decode_args("compressed_decode_weighted", B, Hq, Hkv, d, rows, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, out,
-                     dev_status, row_weight)
-        scale = 0.0 if softmax_scale is None else float(softmax_scale)   # 0: the library's 1/sqrt(d)
-        return int(lib().sonic_compressed_decode_weighted(
-            B, Hq, Hkv, d, int(max_ctx), _ptr(k_cache), _ptr(v_cache), _ptr(cache_row_off), _ptr(cache_row_cap), _ptr(cache_len),
-            _ptr(q), _ptr(k_new), _ptr(v_new), scale, _ptr(out), _ptr(row_weight), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream)))
+    B, Hq, d = q.shape
+    Hkv, rows = k_new.shape[1], k_cache.shape[0]
+    planes = [("k_cache", k_cache, _BF16, (rows, Hkv, d)), ("v_cache", v_cache, _BF16, (rows, Hkv, d))]
+    return _pass("compressed_decode_weighted", lib().sonic_compressed_decode_weighted, stream, (B, Hq, Hkv, d, int(max_ctx)), [
+        *_decode_tensors(planes, B, Hq, Hkv, d, rows, cache_row_off, cache_row_cap, cache_len, q, k_new, v_new, softmax_scale, out,
+                         row_weight, workspace), ("dev_status", dev_status, _I32, None)])
 
 
 def kv_compact_weights(cu_seqlens, key_weight, cache_row_off, cache_len, keep_idx, row_weight, dev_status, max_rows: int,
                        stream=None) -> int:
     """The prefill's key_weight fp32 [T] to the rows a compaction kept: row_weight fp32 [rows], keep_idx int32 [rows]."""
-    with _on_one_device(cu_seqlens, key_weight, cache_row_off, cache_len, keep_idx, row_weight, dev_status):
-        B = cu_seqlens.numel() - 1
-        _types(cu_seqlens=(cu_seqlens, _I32), key_weight=(key_weight, _F32), cache_row_off=(cache_row_off, _I64),
-               cache_len=(cache_len, _I32), keep_idx=(keep_idx, _I32), row_weight=(row_weight, _F32), dev_status=(dev_status, _I32))
-        _shapes("kv_compact_weights", key_weight=(key_weight, (None,)), cache_row_off=(cache_row_off, (B,)),
-                cache_len=(cache_len, (B,)), keep_idx=(keep_idx, tuple(row_weight.shape)))
-        return int(lib().sonic_kv_compact_weights(
-            B, key_weight.numel(), int(max_rows), _ptr(cu_seqlens), _ptr(key_weight), _ptr(cache_row_off), _ptr(cache_len),
-            _ptr(keep_idx), _ptr(row_weight), _ptr(dev_status), _stream(stream)))
+    B = cu_seqlens.numel() - 1
+    return _pass("kv_compact_weights", lib().sonic_kv_compact_weights, stream, (B, key_weight.numel(), int(max_rows)), [
+        ("cu_seqlens", cu_seqlens, _I32, None), ("key_weight", key_weight, _F32, None), ("cache_row_off", cache_row_off, _I64, (B,)),
+        ("cache_len", cache_len, _I32, (B,)), ("keep_idx", keep_idx, _I32, row_weight.shape), ("row_weight", row_weight, _F32, None),
+        ("dev_status", dev_status, _I32, None)])
 
 
 def cache_evict_workspace_bytes(batch: int, max_rows: int) -> int:
@@ -472,31 +464,17 @@ def cache_evict(k_cache, v_cache, cache_row_off, cache_len, row_weight, keep_hea
     [rows,Hkv,d], or codes [rows,Hkv,d/2] with k_scale/v_scale [rows,Hkv,d/32].  Without k_out the rows move down in
     place; with it (and v_out, the scales, out_row_off, out_row_cap, out_len, out_weight) they go to another cache.
     keep_idx int32 [rows of the cache written] or None: the kept rows' places before the call."""
-    with _on_one_device(k_cache, v_cache, cache_row_off, cache_len, row_weight, keep_head, keep_tail, budget, workspace, dev_status,
-                        k_scale, v_scale, k_out, v_out, k_scale_out, v_scale_out, out_row_off, out_row_cap, out_len, out_weight,
-                        keep_idx):
-        rows, Hkv, width = k_cache.shape
-        B = cache_row_off.numel()
-        if k_scale is None:
-            d = width
-            _types(k_cache=(k_cache, _BF16), v_cache=(v_cache, _BF16), k_out=(k_out, _BF16), v_out=(v_out, _BF16))
-            _shapes("cache_evict", v_cache=(v_cache, (rows, Hkv, d)))
-        else:
-            d = 2 * width
-            _q4_rows("cache_evict", Hkv, d, k_cache, k_scale, v_cache, v_scale)
-            _types(k_out=(k_out, _U8), v_out=(v_out, _U8), k_scale_out=(k_scale_out, _U8), v_scale_out=(v_scale_out, _U8))
-        n = rows if k_out is None else k_out.shape[0]
-        _types(cache_row_off=(cache_row_off, _I64), cache_len=(cache_len, _I32), row_weight=(row_weight, _F32),
-               keep_head=(keep_head, _I32), keep_tail=(keep_tail, _I32), budget=(budget, _I32), out_row_off=(out_row_off, _I64),
-               out_row_cap=(out_row_cap, _I32), out_len=(out_len, _I32), out_weight=(out_weight, _F32), keep_idx=(keep_idx, _I32),
-               dev_status=(dev_status, _I32))
-        _shapes("cache_evict", row_weight=(row_weight, (rows,)), cache_len=(cache_len, (B,)), keep_head=(keep_head, (B,)),
-                keep_tail=(keep_tail, (B,)), budget=(budget, (B,)), k_out=(k_out, (n, Hkv, width)), v_out=(v_out, (n, Hkv, width)),
-                k_scale_out=(k_scale_out, (n, Hkv, d // 32)), v_scale_out=(v_scale_out, (n, Hkv, d // 32)),
-                out_row_off=(out_row_off, (B,)), out_row_cap=(out_row_cap, (B,)), out_len=(out_len, (B,)),
-                out_weight=(out_weight, (n,)), keep_idx=(keep_idx, (n,)))
-        return int(lib().sonic_cache_evict(
-            B, int(max_rows), Hkv, d, _ptr(k_cache), _ptr(k_scale), _ptr(v_cache), _ptr(v_scale), _ptr(cache_row_off), _ptr(cache_len),
-            _ptr(row_weight), _ptr(keep_head), _ptr(keep_tail), _ptr(budget), _ptr(k_out), _ptr(k_scale_out), _ptr(v_out),
-            _ptr(v_scale_out), _ptr(out_row_off), _ptr(out_row_cap), _ptr(out_len), _ptr(out_weight), _ptr(keep_idx), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream)))
+    rows, Hkv, width = k_cache.shape
+    B = cache_row_off.numel()
+    kind, d = (_BF16, width) if k_scale is None else (_U8, 2 * width)
+    n = rows if k_out is None else k_out.shape[0]
+    row, scales, new_row, new_scales = (rows, Hkv, width), (rows, Hkv, d // 32), (n, Hkv, width), (n, Hkv, d // 32)
+    return _pass("cache_evict", lib().sonic_cache_evict, stream, (B, int(max_rows), Hkv, d), [
+        ("k_cache", k_cache, kind, None), ("k_scale", k_scale, _U8, scales), ("v_cache", v_cache, kind, row),
+        ("v_scale", v_scale, _U8, scales), ("cache_row_off", cache_row_off, _I64, None), ("cache_len", cache_len, _I32, (B,)),
+        ("row_weight", row_weight, _F32, (rows,)), ("keep_head", keep_head, _I32, (B,)), ("keep_tail", keep_tail, _I32, (B,)),
+        ("budget", budget, _I32, (B,)), ("k_out", k_out, kind, new_row), ("k_scale_out", k_scale_out, _U8, new_scales),
+        ("v_out", v_out, kind, new_row), ("v_scale_out", v_scale_out, _U8, new_scales), ("out_row_off", out_row_off, _I64, (B,)),
+        ("out_row_cap", out_row_cap, _I32, (B,)), ("out_len", out_len, _I32, (B,)), ("out_weight", out_weight, _F32, (n,)),
+        ("keep_idx", keep_idx, _I32, (n,)), ("workspace", workspace, workspace.dtype, None),
+        _number(workspace.numel() * workspace.element_size()), ("dev_status", dev_status, _I32, None)])
