@@ -208,7 +208,10 @@ hipError_t launch_compact(int batch, int total_tokens, int max_seqlen, int Hkv, 
                           hipStream_t stream) {
   const int chunks = max(1, (max_seqlen + kCompactChunk - 1) / kCompactChunk);
   const long cb = static_cast<long>(chunks) * batch;
-  const int slices = static_cast<int>(max(1L, min(static_cast<long>(kCompactMaxSlices), (2048 + cb - 1) / cb)));
+  // (a slice reads the roles before its chunk again; of 4-bit rows it stores a quarter, and half as many are faster: 4
+  // requests of 40,320 tokens 28.4 us, with 2,048 workgroups 30.8)
+  const long want = kscale == nullptr ? 2048 : 1024;
+  const int slices = static_cast<int>(max(1L, min(static_cast<long>(kCompactMaxSlices), (want + cb - 1) / cb)));
   dim3 grid(chunks, batch, slices);
 #define GO(DD, Q4)                                                                                              \
   compact_kernel<DD, Q4><<<grid, dim3(kCompactThreads), 0, stream>>>(cu, role, k, v, kc, vc, kscale, vscale, row_off, \

@@ -22,6 +22,8 @@ constexpr int kSelectRows = 8;                              // consecutive rows 
 constexpr int kSelectChunk = kSelectThreads * kSelectRows;
 constexpr int kMoveThreads = 256;
 constexpr int kMoveUnroll = 4;
+constexpr int kWalkThreads = 1024;
+constexpr int kWalkUnroll = 8;
 
 // A request's rows, cut into head, middle and tail.
 struct EvictReq {
@@ -45,42 +47,39 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// The digit of the radix search's pass at `shift`, counted from above: writes the digit that holds the `need`-th key, how
-// many of its keys are wanted, and how many it has.  kCopies histograms (a lane has its own: weights share their
-// exponents, and 64 lanes adding to one word take turns) are added up first.
-constexpr int kCopies = 16, kCopyStride = 257;
+// A pass of the radix search: 2,048 bins, a quarter of the lanes adding to a copy of their own (weights share their
+// exponents, and lanes that add to one word take turns).  find_digit adds the copies up and writes the digit that
+// holds the `need`-th key from above, how many of its keys are wanted, and how many it has; the copies are clear again.
+constexpr int kDigitBits = 11, kBins = 1 << kDigitBits, kCopies = 4;
+static_assert(kBins == 2 * kSelectThreads, "a thread adds up two bins");
 struct Digit {
   int digit, rest, count;
 };
-__device__ __forceinline__ void find_digit(const int *copies, int *hist, int need, Digit *found) {
-  if (threadIdx.x < 256) {
-    int sum = 0;
+__device__ __forceinline__ void find_digit(int *copies, int need, Digit *found, int *lds) {
+  // thread t has the bins kBins - 1 - 2 t and the one below
+  int h[2] = {0, 0};
+  const int top = kBins - 1 - 2 * threadIdx.x;
 #pragma unroll
-    for (int c = 0; c < kCopies; ++c) sum += copies[c * kCopyStride + threadIdx.x];
-    hist[threadIdx.x] = sum;
+  for (int c = 0; c < kCopies; ++c) {
+    int2 *pair = reinterpret_cast<int2 *>(copies + c * kBins + top - 1);
+    const int2 x = *pair;
+    *pair = make_int2(0, 0);
+    h[0] += x.y;
+    h[1] += x.x;
   }
-  __syncthreads();
-  if (threadIdx.x < kWave) {
-    // lane l holds digits 255 - 4 l down to 252 - 4 l
-    int h[4], sum = 0;
+  int total;
+  int above = block_int_scan<kSelectThreads>(h[0] + h[1], &total, lds);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum += h[i] = hist[255 - 4 * threadIdx.x - i];
-    int above = wave_scan(sum) - sum;
-    if (above < need && above + sum >= need) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (above < need && above + h[i] >= need) *found = Digit{static_cast<int>(255 - 4 * threadIdx.x - i), need - above, h[i]};
-        above += h[i];
-      }
-    }
+  for (int i = 0; i < 2; ++i) {
+    if (above < need && above + h[i] >= need) *found = Digit{top - i, need - above, h[i]};
+    above += h[i];
   }
   __syncthreads();
 }
 
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, EvictWs ws) {
   __shared__ int lds[2 * (kSelectThreads / kWave)];
-  __shared__ int copies[kCopies * kCopyStride];
-  __shared__ int hist[256];
+  __shared__ __align__(8) int copies[kCopies * kBins];
   __shared__ int s_ok, s_first;
   __shared__ Digit s_digit;
   const int b = blockIdx.x;
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, Evi
     EvictReq r;
     bad |= evict_check(j, c, &r) != 0;
   }
-  for (int i = threadIdx.x; i < kCopies * kCopyStride; i += kSelectThreads) copies[i] = 0;
+  for (int i = threadIdx.x; i < kCopies * kBins; i += kSelectThreads) copies[i] = 0;
   if (threadIdx.x == 0) s_first = own.kept;
   bad = __syncthreads_or(bad);
   if (own_code != 0 && threadIdx.x == 0) raise_status(c.status, own_code);
@@ -129,34 +128,45 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, Evi
     threshold = 0xFFFFFFFEu;   // none: only head and tail are above
     int need = take;
     uint32_t prefix = 0;
-    for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
-      int *const copy = copies + (threadIdx.x % kCopies) * kCopyStride;
-      for (int base = 0; base < hi; base += kSelectChunk) {
-        uint32_t key[kSelectRows];
-        if (base == 0) {
+    int *const copy = copies + (threadIdx.x % kCopies) * kBins;
+    for (int shift = 32 - kDigitBits, bits = kDigitBits; need > 0; bits = min(kDigitBits, shift), shift -= bits) {
+      const uint32_t mask = (1u << bits) - 1;
+      auto add = [&](uint32_t key) {
+        if (key - 1u < 0xFFFFFFFEu && (shift + bits == 32 || (key >> (shift + bits)) == prefix)) atomicAdd(&copy[(key >> shift) & mask], 1);
+      };
 #pragma unroll
-          for (int i = 0; i < kSelectRows; ++i) key[i] = first_keys[i];
-        } else {
-          load_keys(base, key);
+      for (int i = 0; i < kSelectRows; ++i) add(first_keys[i]);
+      // the rows behind the first chunk, in an order that needs no sorting out: a batch ahead, whole lines
+      const int begin = max(lo, kSelectChunk);
+      auto load = [&](int base, float (&x)[kSelectRows]) {
+#pragma unroll
+        for (int i = 0; i < kSelectRows; ++i) {
+          const int r = base + i * kSelectThreads + threadIdx.x;
+          x[i] = r < hi ? w[r] : 0.f;
         }
+      };
+      float x[kSelectRows];
+      if (begin < hi) load(begin, x);
+      for (int base = begin; base < hi; base += kSelectChunk) {
+        float ahead[kSelectRows];
+        if (base + kSelectChunk < hi) load(base + kSelectChunk, ahead);
 #pragma unroll
         for (int i = 0; i < kSelectRows; ++i)
-          if (key[i] - 1u < 0xFFFFFFFEu && (shift == 24 || (key[i] >> (shift + 8)) == prefix))
-            atomicAdd(&copy[(key[i] >> shift) & 255], 1);
+          if (base + i * kSelectThreads + static_cast<int>(threadIdx.x) < hi) add(weight_key(x[i]));
+#pragma unroll
+        for (int i = 0; i < kSelectRows; ++i) x[i] = ahead[i];
       }
       __syncthreads();
-      find_digit(copies, hist, need, &s_digit);
+      find_digit(copies, need, &s_digit, lds);
       const Digit d = s_digit;
-      prefix = prefix << 8 | static_cast<uint32_t>(d.digit);
+      prefix = prefix << bits | static_cast<uint32_t>(d.digit);
       threshold = prefix << shift;
       rest = need = d.rest;
       if (d.rest == d.count) {   // all of the digit's keys are kept: no need to tell them apart
         threshold -= 1;          // (not below 0: a key is above 0)
         rest = need = 0;
-      } else if (shift > 0) {
-        for (int i = threadIdx.x; i < kCopies * kCopyStride; i += kSelectThreads) copies[i] = 0;
-        __syncthreads();
       }
+      if (shift == 0) break;
     }
   }
 
@@ -164,12 +174,9 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, Evi
   int listed = 0, equal = 0;
   for (int base = 0; base < own.len; base += kSelectChunk) {
     uint32_t key[kSelectRows];
-    if (base == 0) {
 #pragma unroll
-      for (int i = 0; i < kSelectRows; ++i) key[i] = first_keys[i];
-    } else {
-      load_keys(base, key);
-    }
+    for (int i = 0; i < kSelectRows; ++i) key[i] = first_keys[i];
+    if (base + kSelectChunk < own.len) load_keys(base + kSelectChunk, first_keys);   // the next chunk's, ahead
     int sure = 0, ties = 0;
 #pragma unroll
     for (int i = 0; i < kSelectRows; ++i) {
@@ -255,30 +262,38 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictCall c, EvictWs
 template <typename UNIT>
 __device__ __forceinline__ void walk_down(UNIT *plane, size_t row0, int row_units, int unit0, int units, const int32_t *list,
                                           int first, int kept) {
-  const int rows = kMoveThreads / units;   // rows that the threads cover at once
+  const int rows = kWalkThreads / units;   // rows that the threads cover at once
   const int i = threadIdx.x / units, u = threadIdx.x % units;
-  const bool active = i < rows;
   UNIT *p = plane + row0 * row_units + unit0 + u;
-  for (int j0 = first; j0 < kept; j0 += rows * kMoveUnroll) {
-    UNIT x[kMoveUnroll];
+  int from[kWalkUnroll];
+  auto look_up = [&](int j0) {
 #pragma unroll
-    for (int n = 0; n < kMoveUnroll; ++n) {
+    for (int n = 0; n < kWalkUnroll; ++n) {
       const int j = j0 + n * rows + i;
-      if (active && j < kept) x[n] = p[static_cast<size_t>(list[j]) * row_units];
+      from[n] = i < rows && j < kept ? list[j] : -1;
     }
-    __syncthreads();   // the batch is loaded by every thread: rows below j0 + rows * kMoveUnroll may be overwritten
+  };
+  look_up(first);
+  for (int j0 = first; j0 < kept; j0 += rows * kWalkUnroll) {
+    UNIT x[kWalkUnroll];
+    int to[kWalkUnroll];
 #pragma unroll
-    for (int n = 0; n < kMoveUnroll; ++n) {
-      const int j = j0 + n * rows + i;
-      if (active && j < kept) p[static_cast<size_t>(j) * row_units] = x[n];
+    for (int n = 0; n < kWalkUnroll; ++n) {
+      to[n] = from[n] < 0 ? -1 : j0 + n * rows + i;
+      if (from[n] >= 0) x[n] = p[static_cast<size_t>(from[n]) * row_units];
     }
+    look_up(j0 + rows * kWalkUnroll);
+    __syncthreads();   // the batch is loaded by every thread: rows below j0 + rows * kWalkUnroll may be overwritten
+#pragma unroll
+    for (int n = 0; n < kWalkUnroll; ++n)
+      if (to[n] >= 0) p[static_cast<size_t>(to[n]) * row_units] = x[n];
   }
 }
 
 // In place.  Grid (columns, requests): the columns of K, of V, of the scales of K and V, and the weights.
 template <typename SCALE>
-__global__ __launch_bounds__(kMoveThreads) void move_in_place_kernel(EvictCall c, EvictWs ws, int row_units, int col_units,
-                                                                     int scale_units) {
+__global__ __launch_bounds__(kWalkThreads) void move_in_place_kernel(EvictCall c, EvictWs ws, int row_units, int col_units,
+                                                                     int scale_units, int scale_col_units) {
   if (ws.ctrl[0] == 0) return;
   const int b = blockIdx.y;
   const int kept = ws.req[b].x, first = ws.req[b].y;
@@ -293,16 +308,16 @@ __global__ __launch_bounds__(kMoveThreads) void move_in_place_kernel(EvictCall c
     return;
   }
   col -= 2 * cols;
-  const int scale_cols = (scale_units + kMoveThreads - 1) / kMoveThreads;
+  const int scale_cols = scale_units > 0 ? (scale_units + scale_col_units - 1) / scale_col_units : 0;
   if (col < 2 * scale_cols) {
     SCALE *plane = reinterpret_cast<SCALE *>(const_cast<uint8_t *>(col < scale_cols ? c.ks : c.vs));
-    const int unit0 = col % scale_cols * kMoveThreads;
-    walk_down(plane, row0, scale_units, unit0, min(kMoveThreads, scale_units - unit0), list, first, kept);
+    const int unit0 = col % scale_cols * scale_col_units;
+    walk_down(plane, row0, scale_units, unit0, min(scale_col_units, scale_units - unit0), list, first, kept);
     return;
   }
   walk_down(c.row_weight, row0, 1, 0, 1, list, first, kept);
   if (c.keep_idx != nullptr)
-    for (int j = threadIdx.x; j < kept; j += kMoveThreads) c.keep_idx[row0 + j] = list[j];
+    for (int j = threadIdx.x; j < kept; j += kWalkThreads) c.keep_idx[row0 + j] = list[j];
   if (threadIdx.x == 0) c.cache_len[b] = kept;
 }
 
@@ -314,10 +329,16 @@ static void launch_moves(const EvictCall &c, const EvictWs &ws, int row_units, i
                                               std::max(16L, 4096L / c.batch)));
     move_kernel<SCALE><<<dim3(chunks, c.batch), dim3(kMoveThreads), 0, stream>>>(c, ws, row_units, scale_units);
   } else {
-    const int col_units = 4;   // 64 bytes
-    const int cols = (row_units + col_units - 1) / col_units, scale_cols = (scale_units + kMoveThreads - 1) / kMoveThreads;
-    move_in_place_kernel<SCALE><<<dim3(2 * cols + 2 * scale_cols + 1, c.batch), dim3(kMoveThreads), 0, stream>>>(
-        c, ws, row_units, col_units, scale_units);
+    // Columns of 128 bytes, or of 64 where that makes fewer than 64 workgroups.  An iteration of a workgroup moves
+    // kWalkThreads * kWalkUnroll units and takes its time whatever their number; narrower columns than that have every
+    // line fetched several times (1 request of 30,000 bf16 rows of 8 heads of 128 to 20,000: 16 bytes 215 us, 32 134,
+    // 64 118, 128 125; 4 of 7,552 rows of 4 heads to 7,000: 131, 79, 55, 49).
+    int col_units = 8;
+    if (2L * c.batch * ((row_units + col_units - 1) / col_units) < 64) col_units = 4;
+    const int scale_col_units = std::max(1, std::min(scale_units, c.batch < 16 ? 2 : 8));
+    const int cols = (row_units + col_units - 1) / col_units, scale_cols = (scale_units + scale_col_units - 1) / scale_col_units;
+    move_in_place_kernel<SCALE><<<dim3(2 * cols + 2 * scale_cols + 1, c.batch), dim3(kWalkThreads), 0, stream>>>(
+        c, ws, row_units, col_units, scale_units, scale_col_units);
   }
 }
 

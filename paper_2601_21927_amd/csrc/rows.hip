@@ -79,20 +79,44 @@ __global__ __launch_bounds__(kRowThreads) void compact_weights_kernel(
 
 // After a decode step that kept its scores: row r's weight grows by the mean over the q-heads of
 // exp2(score - normaliser); the appended row's starts there.  Requests the step did not advance (fresh 0) are left
-// alone.  One thread owns a row and adds the heads in order, so the sums do not depend on timing.
-__global__ __launch_bounds__(kRowThreads) void add_weights_kernel(const int64_t *__restrict__ row_off, DecodeRows rows,
-                                                                  float *__restrict__ row_weight, int Hq, float inv_heads) {
+// alone.  A workgroup has 64 rows, a wave a quarter of the heads (kHeadUnroll of them in flight, requested before the
+// request's length is known: every row of the grid has room), and the waves' sums are added in order, so they do not
+// depend on timing.
+constexpr int kWeightRows = kWave, kWeightWaves = 4, kHeadUnroll = 8;
+__global__ __launch_bounds__(kWeightRows *kWeightWaves) void add_weights_kernel(const int64_t *__restrict__ row_off, DecodeRows rows,
+                                                                                float *__restrict__ row_weight, int Hq,
+                                                                                float inv_heads) {
+  __shared__ float part[kWeightWaves][kWeightRows];
   const int b = blockIdx.y;
   const int n = rows.fresh[b];
-  const int r = blockIdx.x * kRowThreads + threadIdx.x;
-  if (r >= n) return;
-  const float *score = rows.scores + static_cast<size_t>(b) * Hq * rows.stride + r;
+  const int64_t off = row_off[b];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = blockIdx.x * kWeightRows + lane;
+  // (with many workgroups the traffic of those past the request's end counts for more than the round trip)
+  if (gridDim.x * gridDim.y > 2048 && static_cast<int>(blockIdx.x) * kWeightRows >= n) return;
+  const float *score = rows.scores + static_cast<size_t>(b) * Hq * rows.stride + min(static_cast<size_t>(r), rows.stride - 1);
   const float *lse = rows.lse + static_cast<size_t>(b) * Hq;
-  float *w = row_weight + row_off[b] + r;
-  const float old = r == n - 1 ? 0.f : *w;
+  const int per = (Hq + kWeightWaves - 1) / kWeightWaves, h0 = wave * per, h1 = min(Hq, h0 + per);
   float sum = 0.f;
-#pragma unroll 8
-  for (int h = 0; h < Hq; ++h) sum += __builtin_amdgcn_exp2f(score[h * rows.stride] - lse[h]);
+  for (int h = h0; h < h1; h += kHeadUnroll) {
+    float s[kHeadUnroll], l[kHeadUnroll];
+#pragma unroll
+    for (int i = 0; i < kHeadUnroll; ++i) {
+      const int hh = min(h + i, h1 - 1);
+      s[i] = score[hh * rows.stride];
+      l[i] = lse[hh];
+    }
+#pragma unroll
+    for (int i = 0; i < kHeadUnroll; ++i)
+      if (h + i < h1) sum += __builtin_amdgcn_exp2f(s[i] - l[i]);
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave > 0 || r >= n) return;
+  float *w = row_weight + off + r;
+  const float old = r == n - 1 ? 0.f : *w;
+#pragma unroll
+  for (int i = 1; i < kWeightWaves; ++i) sum += part[i][lane];
   *w = fmaf(sum, inv_heads, old);
 }
 
@@ -120,7 +144,7 @@ hipError_t launch_compact_weights(int batch, int total_tokens, int max_rows, con
 
 hipError_t launch_add_weights(int batch, int Hq, int max_ctx, const int64_t *row_off, const DecodeRows &rows, float *row_weight,
                               hipStream_t stream) {
-  add_weights_kernel<<<dim3((max_ctx + kRowThreads - 1) / kRowThreads, batch), dim3(kRowThreads), 0, stream>>>(
+  add_weights_kernel<<<dim3((max_ctx + kWeightRows - 1) / kWeightRows, batch), dim3(kWeightRows * kWeightWaves), 0, stream>>>(
       row_off, rows, row_weight, Hq, 1.f / static_cast<float>(Hq));
   return hipGetLastError();
 }
