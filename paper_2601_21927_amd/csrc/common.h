@@ -217,7 +217,8 @@ struct DecodeWs {
 struct DecodeRows {
   uint8_t *ks;        // 4-bit rows: scale bytes of K and V, [rows][Hkv][D / 32]
   uint8_t *vs;
-  float *scores;      // [B][Hq][stride] log2-domain scores of every context row
+  float *scores;      // [B][stride / 16][Hq][16] log2-domain scores of every context row: a kv-head's G q-heads of 16 rows
+                      // are G * 64 bytes in a row where they are stored, and all heads of them where they are added up
   float *lse;         // [B][Hq] log2-domain softmax normaliser
   int32_t *fresh;     // [B] context rows of the requests that this call advanced, 0 for the others
   size_t stride;      // rows a request's scores have room for, a multiple of 16

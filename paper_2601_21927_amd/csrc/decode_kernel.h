@@ -471,7 +471,7 @@ __global__ __launch_bounds__(NW * kWave, Q4 ? 4 : 2) void decode_kernel(
   const int tr_swz = tr_row & VSWZ;
 
   // Scores of rows r0 .. r0 + 15 to probabilities, the operand of the value product.
-  float *const score_row = SCORED ? rows.scores + (static_cast<size_t>(b) * Hq + kvh * G + col) * rows.stride + 4 * quarter : nullptr;
+  float *const score_row = SCORED ? rows.scores + static_cast<size_t>(b) * Hq * rows.stride + (kvh * G + col) * 16 + 4 * quarter : nullptr;
   auto soften = [&](const f32x4 &sacc, int r0, uint32_t roles) {
     // lane (col, quarter) holds rows r0 + 4*quarter + i of column col
     float x[4];
@@ -485,7 +485,7 @@ __global__ __launch_bounds__(NW * kWave, Q4 ? 4 : 2) void decode_kernel(
       mloc = fmaxf(mloc, x[i]);
     }
     if constexpr (SCORED) {   // one store a group, which the waits of the pipeline count
-      if (col < G) *reinterpret_cast<f32x4 *>(score_row + r0) = f32x4{x[0], x[1], x[2], x[3]};
+      if (col < G) *reinterpret_cast<f32x4 *>(score_row + static_cast<size_t>(r0) * Hq) = f32x4{x[0], x[1], x[2], x[3]};
     }
     mloc = pair32_max(pair16_max(mloc));
     if (__any(mloc > m_run + 8.f)) {   // rescale only when the max grows by more than 2^8
@@ -776,7 +776,7 @@ __global__ __launch_bounds__(NW * kWave, Q4 ? 4 : 2) void decode_kernel(
         if (col < G)
 #pragma unroll
           for (int t = 0; t < 2; ++t)   // (a row's scores have room up to a multiple of 16)
-            if (r0 + 16 * t < r_end) *reinterpret_cast<f32x4 *>(score_row + r0 + 16 * t) = s[t] * scale_log2;
+            if (r0 + 16 * t < r_end) *reinterpret_cast<f32x4 *>(score_row + static_cast<size_t>(r0 + 16 * t) * Hq) = s[t] * scale_log2;
       }
       float mloc = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
       mloc = pair32_max(pair16_max(mloc)) * scale_log2;

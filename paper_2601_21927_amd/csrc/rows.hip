@@ -79,45 +79,55 @@ __global__ __launch_bounds__(kRowThreads) void compact_weights_kernel(
 
 // After a decode step that kept its scores: row r's weight grows by the mean over the q-heads of
 // exp2(score - normaliser); the appended row's starts there.  Requests the step did not advance (fresh 0) are left
-// alone.  A workgroup has 64 rows, a wave a quarter of the heads (kHeadUnroll of them in flight, requested before the
-// request's length is known: every row of the grid has room), and the waves' sums are added in order, so they do not
-// depend on timing.
-constexpr int kWeightRows = kWave, kWeightWaves = 4, kHeadUnroll = 8;
-__global__ __launch_bounds__(kWeightRows *kWeightWaves) void add_weights_kernel(const int64_t *__restrict__ row_off, DecodeRows rows,
-                                                                                float *__restrict__ row_weight, int Hq,
-                                                                                float inv_heads) {
-  __shared__ float part[kWeightWaves][kWeightRows];
+// alone.  A wave takes K blocks of 16 rows: lane l has rows 4 (l % 4) .. + 3 of heads l / 4, l / 4 + 16, .., and the
+// lanes' sums are added by exchanges in a fixed order, so they do not depend on timing.
+constexpr int kWeightWaves = 4;
+template <int K>
+__global__ __launch_bounds__(kWave *kWeightWaves) void add_weights_kernel(const int64_t *__restrict__ row_off, DecodeRows rows,
+                                                                          float *__restrict__ row_weight, int Hq, float inv_heads) {
   const int b = blockIdx.y;
   const int n = rows.fresh[b];
   const int64_t off = row_off[b];
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int r = blockIdx.x * kWeightRows + lane;
-  // (with many workgroups the traffic of those past the request's end counts for more than the round trip)
-  if (gridDim.x * gridDim.y > 2048 && static_cast<int>(blockIdx.x) * kWeightRows >= n) return;
-  const float *score = rows.scores + static_cast<size_t>(b) * Hq * rows.stride + min(static_cast<size_t>(r), rows.stride - 1);
+  const int lane = threadIdx.x % kWave;
+  const int r0 = (blockIdx.x * kWeightWaves + static_cast<int>(threadIdx.x) / kWave) * (16 * K);
+  // K = 1, few workgroups: the scores are requested before the request's length is known (its blocks have room)
+  if (K > 1 && r0 >= n) return;
   const float *lse = rows.lse + static_cast<size_t>(b) * Hq;
-  const int per = (Hq + kWeightWaves - 1) / kWeightWaves, h0 = wave * per, h1 = min(Hq, h0 + per);
-  float sum = 0.f;
-  for (int h = h0; h < h1; h += kHeadUnroll) {
-    float s[kHeadUnroll], l[kHeadUnroll];
+  const float *scores = rows.scores + static_cast<size_t>(b) * Hq * rows.stride + 4 * (lane % 4);
+  f32x4 sum[K] = {};
+  for (int h0 = 0; h0 < Hq; h0 += 16) {
+    const bool in = h0 + lane / 4 < Hq;
+    const int h = in ? h0 + lane / 4 : 0;
+    const float l = lse[h];
+    f32x4 s[K];
 #pragma unroll
-    for (int i = 0; i < kHeadUnroll; ++i) {
-      const int hh = min(h + i, h1 - 1);
-      s[i] = score[hh * rows.stride];
-      l[i] = lse[hh];
+    for (int k = 0; k < K; ++k) {
+      const size_t blk = min(static_cast<size_t>(r0 / 16 + k), rows.stride / 16 - 1);
+      s[k] = *reinterpret_cast<const f32x4 *>(scores + (blk * Hq + h) * 16);
     }
 #pragma unroll
-    for (int i = 0; i < kHeadUnroll; ++i)
-      if (h + i < h1) sum += __builtin_amdgcn_exp2f(s[i] - l[i]);
-  }
-  part[wave][lane] = sum;
-  __syncthreads();
-  if (wave > 0 || r >= n) return;
-  float *w = row_weight + off + r;
-  const float old = r == n - 1 ? 0.f : *w;
+    for (int k = 0; k < K; ++k)
 #pragma unroll
-  for (int i = 1; i < kWeightWaves; ++i) sum += part[i][lane];
-  *w = fmaf(sum, inv_heads, old);
+      for (int e = 0; e < 4; ++e) sum[k][e] += in ? __builtin_amdgcn_exp2f(s[k][e] - l) : 0.f;
+  }
+  if (r0 >= n) return;
+  const int r = r0 + lane;   // lane 16 k + 4 i + e: element e of the lanes i of block k
+  const bool mine = lane < 16 * K && r < n;
+  float *w = row_weight + off + r;
+  const float old = mine && r < n - 1 ? *w : 0.f;
+  float total = 0.f;
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float x = sum[k][e];
+      x += __shfl_xor(x, 4);
+      x += __shfl_xor(x, 8);
+      x = pair32_add(pair16_add(x));
+      const float y = __shfl(x, lane / 4 % 4);
+      if (lane / 16 == k && lane % 4 == e) total = y;
+    }
+  if (mine) *w = fmaf(total, inv_heads, old);
 }
 
 hipError_t launch_expand_q4(int batch, int max_rows, int Hkv, int D, const uint8_t *kc, const uint8_t *ks, const uint8_t *vc,
@@ -144,8 +154,12 @@ hipError_t launch_compact_weights(int batch, int total_tokens, int max_rows, con
 
 hipError_t launch_add_weights(int batch, int Hq, int max_ctx, const int64_t *row_off, const DecodeRows &rows, float *row_weight,
                               hipStream_t stream) {
-  add_weights_kernel<<<dim3((max_ctx + kWeightRows - 1) / kWeightRows, batch), dim3(kWeightRows * kWeightWaves), 0, stream>>>(
-      row_off, rows, row_weight, Hq, 1.f / static_cast<float>(Hq));
+  const float inv = 1.f / static_cast<float>(Hq);
+  auto blocks = [&](int k) { return (max_ctx + 16 * k * kWeightWaves - 1) / (16 * k * kWeightWaves); };
+  if (static_cast<long>(blocks(1)) * batch <= 1024)
+    add_weights_kernel<1><<<dim3(blocks(1), batch), dim3(kWave * kWeightWaves), 0, stream>>>(row_off, rows, row_weight, Hq, inv);
+  else
+    add_weights_kernel<4><<<dim3(blocks(4), batch), dim3(kWave * kWeightWaves), 0, stream>>>(row_off, rows, row_weight, Hq, inv);
   return hipGetLastError();
 }
 
