@@ -208,6 +208,39 @@ def test_captured_eviction_is_replayed_like_an_eager_one():
         cycle()
 
 
+@pytest.mark.parametrize("q4", [True, False])
+def test_rows_past_four_gigabytes(q4):
+    H.need_gpu()
+    Hkv, d, n, budget = 8, 128, 300, 120
+    row = Hkv * d // 2 if q4 else Hkv * d * 2
+    first = (1 << 32) // row + 77
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    shape = [(first + n, Hkv, d // 2), (first + n, Hkv, d // 32)] * 2 if q4 else [(first + n, Hkv, d)] * 2
+    planes = [torch.zeros(s, dtype=torch.uint8 if q4 else torch.bfloat16, device="cuda") for s in shape]
+    for x in planes:
+        x[first:] = torch.randint(0, 200, x[first:].shape, generator=gen, device="cuda").to(x.dtype)
+    k, ks, v, vs = planes if q4 else (planes[0], None, planes[1], None)
+    w = torch.zeros(first + n, device="cuda")
+    w[first:] = torch.rand(n, generator=gen, device="cuda")
+    before = [x[first:].clone() for x in planes]
+    kept = torch.from_numpy(OE.kept_rows(w[first:].cpu().numpy(), 5, 6, budget)).cuda()
+    off, ln, status = torch.tensor([first], dtype=torch.int64, device="cuda"), i32([n]), i32([0])
+    ws = torch.zeros(sonic.cache_evict_workspace_bytes(1, n), dtype=torch.uint8, device="cuda")
+    lim = (i32([5]), i32([6]), i32([budget]))
+    # to another cache, whose rows lie past 4 GiB too, then in place
+    out = [torch.zeros_like(x) for x in planes]
+    more = dict(k_out=out[0], v_out=out[2 if q4 else 1], out_row_off=off, out_row_cap=i32([n]), out_len=i32([0]), out_weight=torch.zeros_like(w))
+    if q4:
+        more.update(k_scale_out=out[1], v_scale_out=out[3])
+    assert sonic.cache_evict(k, v, off, ln, w, *lim, ws, status, n, k_scale=ks, v_scale=vs, **more) == sonic.OK
+    for x, old in zip(out, before):
+        assert torch.equal(x[first:first + budget], old[kept]) and not x[:first].any()
+    assert sonic.cache_evict(k, v, off, ln, w, *lim, ws, status, n, k_scale=ks, v_scale=vs) == sonic.OK
+    for x, old in zip(planes, before):
+        assert torch.equal(x[first:first + budget], old[kept]) and torch.equal(x[first + budget:], old[budget:]) and not x[:first].any()
+    assert int(ln.item()) == budget and int(status.item()) == 0
+
+
 # ------------------------------------------------------------------ the prefill's key weights
 def test_key_weights_go_to_the_compacted_rows():
     H.need_gpu()

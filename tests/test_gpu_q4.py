@@ -222,7 +222,8 @@ def test_decode_steps(Hq, Hkv, d, q4):
 
 
 @pytest.mark.parametrize("q4", [True, False])
-@pytest.mark.parametrize("lens,Hq,Hkv,d", [([9000], 8, 2, 128), ([40000], 2, 1, 64), ([5000, 3], 7, 1, 128), ([2500, 10, 700, 4000] * 2, 8, 8, 64)])
+@pytest.mark.parametrize("lens,Hq,Hkv,d", [([9000], 8, 2, 128), ([40000], 2, 1, 64), ([5000, 3], 7, 1, 128), ([2500, 10, 700, 4000] * 2, 8, 8, 64),
+                                           ([16500], 8, 8, 128), ([33000], 4, 4, 64)])
 def test_decode_long_contexts(lens, Hq, Hkv, d, q4):
     """Contexts cut into many ranges, and several lengths in one call."""
     H.need_gpu()
@@ -327,9 +328,9 @@ def test_a_nan_key_in_one_range_makes_every_weight_nan(q4):
     rng = np.random.default_rng(14)
     c = Cache(rng, [2048], 2, 1, 64, q4)
     if q4:
-        c.dev.k_scale[256:512] = 255
+        c.dev.k_scale[200:900] = 255
     else:
-        c.dev.k[256:512] = float("nan")
+        c.dev.k[200:900] = float("nan")
     *_, out = c.step(rng, 2)
     assert np.isnan(out).all()
     assert np.isnan(c.dev.row_weight.cpu().numpy()[:2049]).all()
@@ -408,6 +409,41 @@ def test_a_status_word_that_changes_while_calls_run_leaves_the_next_call_right()
     c.dev.length.copy_(i32(c.lens))
     c.dev.row_weight.copy_(torch.from_numpy(c.weight))
     c.check(*c.step(rng, 4))
+
+
+def test_rows_past_four_gigabytes():
+    """Codes, scales and bf16 rows behind the first 4 GiB of their tensors: compaction, step, reading back."""
+    H.need_gpu()
+    rng = np.random.default_rng(20)
+    Hkv, d, n = 8, 128, 70
+    first = (1 << 32) // (Hkv * d // 2) + 1000          # of the codes
+    k, v = normal_bits(rng, n, Hkv, d), normal_bits(rng, n, Hkv, d)
+    off = torch.tensor([first], dtype=torch.int64, device="cuda")
+    planes = [torch.full((first + n + 1, Hkv, w), 255, dtype=torch.uint8, device="cuda") for w in (d // 2, d // 32, d // 2, d // 32)]
+    kc, ks, vc, vs = planes
+    idx, ln, status = torch.zeros(first + n + 1, dtype=torch.int32, device="cuda"), i32([0]), i32([0])
+    cap = i32([n + 1])
+    assert sonic.kv_compact_q4(i32([0, n]), torch.full((n,), 3, dtype=torch.uint8, device="cuda"), bf16_to_device(k), bf16_to_device(v), kc, ks,
+                               vc, vs, off, cap, ln, idx, status, n) == sonic.OK
+    q, kn, vn = (normal_bits(rng, 1, h, d) for h in (16, Hkv, Hkv))
+    out = torch.zeros((1, 16, d), device="cuda")
+    weight = torch.zeros(first + n + 1, device="cuda")
+    ws = torch.zeros(sonic.decode_q4_workspace_bytes(1, 16, d, n + 1, True), dtype=torch.uint8, device="cuda")
+    assert sonic.compressed_decode_q4(kc, ks, vc, vs, off, cap, ln, bf16_to_device(q), bf16_to_device(kn), bf16_to_device(vn), out, ws, status,
+                                      n + 1, row_weight=weight) == sonic.OK
+    kv = [OQ.rounded(np.concatenate(x)) for x in ((k, kn), (v, vn))]
+    want, w = OE.attend(q[0], *kv)
+    assert int(status.item()) == 0 and int(ln.item()) == n + 1
+    assert np.all(np.abs(out[0].cpu().numpy() - want) <= 2 * EPS * np.abs(kv[1]).max())
+    assert np.all(np.abs(weight[first:].cpu().numpy() - w) <= 2 * EPS * w) and not weight[:first].any()
+    assert torch.all(kc[:first] == 255) and torch.all(vs[:first] == 255)
+    # back to bf16 rows that lie past 4 GiB too
+    far = (1 << 32) // (Hkv * d * 2) + 10
+    ko, vo = (torch.zeros((far + n + 1, Hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert sonic.cache_expand_q4(kc, ks, vc, vs, off, cap, i32([0]), ln, ko, vo, torch.tensor([far], dtype=torch.int64, device="cuda"), cap,
+                                 status, n + 1) == sonic.OK
+    for got, values in ((ko, kv[0]), (vo, kv[1])):
+        assert np.array_equal(got[far:].double().cpu().numpy(), values) and not got[:far].any()
 
 
 def test_binding_refusals():
