@@ -2,7 +2,7 @@
 the roundings on the way.
 
 Bars.  A decode output is a convex combination of V values whose probabilities are off by a relative EPS = 2^-15:
-the two bf16 parts of a probability leave 2^-17 of it, the exponential of a 32-bit score of log2 size up to 64 is off
+the bf16 parts of a probability leave 2^-17 of it at most, the exponential of a 32-bit score of log2 size up to 64 is off
 by 64 * 2^-24 / log2(e) and the hardware's 2^-22, and sums of 32-bit values add less; the sum of the probabilities is
 off by as much again.  So |out - exact| <= 2 * EPS * max|V|, and a weight, a mean of such probabilities, is within
 2 * EPS of itself and half a step of the sum it is added to.
