@@ -21,7 +21,7 @@ constexpr int kSelectThreads = 1024;
 constexpr int kSelectRows = 8;                              // consecutive rows of a thread
 constexpr int kSelectChunk = kSelectThreads * kSelectRows;
 constexpr int kMoveThreads = 256;
-constexpr int kMoveUnroll = 4;
+constexpr int kMoveUnroll = 8;   // 64 uneven requests of 8,192 rows at most to half of that: 149 us a pass, with 4 158, with 16 206
 constexpr int kWalkThreads = 1024;
 constexpr int kWalkUnroll = 8;
 
