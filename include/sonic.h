@@ -502,7 +502,9 @@ size_t sonic_decode_q4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32
  * and the attention reads every row, the appended one too, at its 4-bit values.
  *   row_weight   NULL, or device fp32 [rows]: see sonic_compressed_decode_weighted
  * The other arguments, outputs and errors are those of sonic_compressed_decode without
- * row_role; a NaN row makes the outputs it reaches NaN.
+ * row_role; a NaN row makes the outputs it reaches NaN.  The workspace is zero-filled before its
+ * first use, and again before calls of another shape (batch, heads, head_dim, max_ctx); one made for
+ * weights serves calls without them too.
  */
 int32_t sonic_compressed_decode_q4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                    int32_t max_ctx, void *k_cache, void *k_scale, void *v_cache, void *v_scale,
@@ -544,7 +546,8 @@ size_t sonic_decode_weighted_workspace_bytes(int32_t batch, int32_t num_q_heads,
  *                does not know of it: after it the caller sets the rows it wrote.
  * The other arguments, outputs and errors are those of sonic_compressed_decode without
  * row_role; the workspace (sonic_decode_weighted_workspace_bytes) is larger by the scores,
- * batch * num_q_heads * max_ctx floats.
+ * batch * num_q_heads * max_ctx floats, and zero-filled before its first use and before calls of
+ * another shape.
  */
 int32_t sonic_compressed_decode_weighted(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                          int32_t max_ctx, void *k_cache, void *v_cache, const int64_t *cache_row_off,

@@ -20,7 +20,9 @@
 //
 // Q4: the rows go to a 4-bit cache (q4.h).  A thread's unit is the same eight values;
 // four neighbouring lanes hold a block of 32, find its scale with two lane exchanges
-// and store four bytes of codes each, the first of them the scale byte.
+// and store four bytes of codes each, the first of them the scale byte.  Bound like the bf16
+// form by the three round trips before the copy: 30,208 of 161,280 rows, 4 heads of 128,
+// 78 MB, 28.4 us (15 at the rate of a copy).
 #include "common.h"
 #include "q4.h"
 #include "scan.h"

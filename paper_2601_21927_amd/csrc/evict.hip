@@ -3,13 +3,16 @@
 // next-turn step reads (system prompt, Nexus rows, the turn's rows).
 //
 // select_kernel, one workgroup per request: checks the lengths of every request, so that a call is done for all or
-// for none, finds the weight that separates kept from dropped rows by a radix search over the weights' order (four
-// passes of eight bits, histograms in LDS; a few bytes per row, served from L2), and lists the kept rows.  It writes
-// to the workspace only.
-// move_kernel, to another cache: every kept row is read and written once, in parallel over rows.
+// for none, finds the weight that separates kept from dropped rows by a radix search over the weights' order (up to
+// three passes of eleven bits, histograms in LDS; a request's first 8,192 weights stay in registers), and lists the kept
+// rows.  It writes to the workspace only.  Bound by its chain of barriers and round trips: 11 us for 8 requests of 1,328
+// rows, 12 for 4 of 7,552, 39 for one of 30,000, 102 for one of 100,000.
+// move_kernel, to another cache: every kept row is read and written once, in parallel over rows.  Bound by HBM: 64
+// uneven requests of up to 8,192 rows of 8 bf16 heads of 128 (652 MB) 4.8 TB/s.
 // move_in_place_kernel: row j goes down to j from list[j] >= j, so a workgroup that walks the rows upwards, loading a
 // batch before it stores it, never overwrites a row it has yet to read; workgroups split the rows' bytes into
-// columns.  Rows before the first dropped one are not touched.
+// columns.  Rows before the first dropped one are not touched.  64 requests of 4,000 bf16 rows to 2,000: 4.5 TB/s; one
+// request has 32 to 64 columns, each a workgroup that waits for its own loads: 30,000 bf16 rows to 20,000 62 us (2.6 TB/s).
 #include <algorithm>
 
 #include "common.h"
