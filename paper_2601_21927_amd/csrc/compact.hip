@@ -22,7 +22,7 @@
 // four neighbouring lanes hold a block of 32, find its scale with two lane exchanges
 // and store four bytes of codes each, the first of them the scale byte.  Bound like the bf16
 // form by the three round trips before the copy: 30,208 of 161,280 rows, 4 heads of 128,
-// 78 MB, 28.4 us (15 at the rate of a copy).
+// 78 MB, 24 us (15 at the rate of a copy).
 #include "common.h"
 #include "q4.h"
 #include "scan.h"
@@ -211,7 +211,7 @@ hipError_t launch_compact(int batch, int total_tokens, int max_seqlen, int Hkv, 
   const int chunks = max(1, (max_seqlen + kCompactChunk - 1) / kCompactChunk);
   const long cb = static_cast<long>(chunks) * batch;
   // (a slice reads the roles before its chunk again; of 4-bit rows it stores a quarter, and half as many are faster: 4
-  // requests of 40,320 tokens 28.4 us, with 2,048 workgroups 30.8)
+  // requests of 40,320 tokens 42.4 us with their reading back, with 2,048 workgroups 44.8)
   const long want = kscale == nullptr ? 2048 : 1024;
   const int slices = static_cast<int>(max(1L, min(static_cast<long>(kCompactMaxSlices), (want + cb - 1) / cb)));
   dim3 grid(chunks, batch, slices);
