@@ -504,7 +504,7 @@ size_t sonic_decode_q4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32
  * The other arguments, outputs and errors are those of sonic_compressed_decode without
  * row_role; a NaN row makes the outputs it reaches NaN.  The workspace is zero-filled before its
  * first use, and again before calls of another shape (batch, heads, head_dim, max_ctx); one made for
- * weights serves calls without them too.
+ * weights serves calls without them too.  Calls that share one must not run concurrently.
  */
 int32_t sonic_compressed_decode_q4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                    int32_t max_ctx, void *k_cache, void *k_scale, void *v_cache, void *v_scale,
@@ -547,7 +547,7 @@ size_t sonic_decode_weighted_workspace_bytes(int32_t batch, int32_t num_q_heads,
  * The other arguments, outputs and errors are those of sonic_compressed_decode without
  * row_role; the workspace (sonic_decode_weighted_workspace_bytes) is larger by the scores,
  * batch * num_q_heads * max_ctx floats, and zero-filled before its first use and before calls of
- * another shape.
+ * another shape.  Calls that share one must not run concurrently.
  */
 int32_t sonic_compressed_decode_weighted(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                          int32_t max_ctx, void *k_cache, void *v_cache, const int64_t *cache_row_off,
@@ -580,7 +580,7 @@ size_t sonic_cache_evict_workspace_bytes(int32_t batch, int32_t max_rows);
  *   keep_idx       NULL, or device int32 [rows of the cache written]: each kept row's place
  *                  (from 0) in its request before the call
  *   workspace      device, 256-byte aligned, >= sonic_cache_evict_workspace_bytes(B, max_rows);
- *                  contents need no initialisation
+ *                  contents need no initialisation; calls that share one must not run concurrently
  *   dev_status     SONIC_ERR_BAD_LAYOUT for a negative length, head, tail or budget, or a length
  *                  above max_rows; SONIC_ERR_CAPACITY when more rows are kept than out_row_cap[b];
  *                  then (as with any pending status) nothing is written for any request

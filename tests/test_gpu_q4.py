@@ -23,7 +23,8 @@ from tests import gpu_helpers as H
 pytestmark = pytest.mark.gpu
 
 EPS = 2.0 ** -15
-HEADS = [(4, 2, 64), (8, 1, 64), (28, 4, 128), (32, 8, 128), (5, 5, 64), (6, 3, 128), (21, 7, 128), (12, 2, 64), (5, 1, 128)]
+HEADS = [(4, 2, 64), (8, 1, 64), (28, 4, 128), (32, 8, 128), (5, 5, 64), (6, 3, 128), (21, 7, 128), (12, 2, 64), (5, 1, 128),
+         (40, 8, 64), (3, 1, 128)]
 
 
 def i32(a):
@@ -234,7 +235,8 @@ def test_decode_long_contexts(lens, Hq, Hkv, d, q4):
 
 
 @pytest.mark.parametrize("q4", [True, False])
-@pytest.mark.parametrize("B,Hq,Hkv,d,top", [(64, 8, 4, 64, 2300), (40, 8, 8, 128, 2100), (33, 16, 8, 64, 400), (300, 4, 1, 64, 90)])
+@pytest.mark.parametrize("B,Hq,Hkv,d,top", [(64, 8, 4, 64, 2300), (40, 8, 8, 128, 2100), (64, 28, 4, 128, 2048), (33, 16, 8, 64, 400), (300, 4, 1, 64, 90),
+                                             (130, 8, 8, 64, 200)])
 def test_decode_many_requests(B, Hq, Hkv, d, top, q4):
     """256 and more pairs: one range a pair, and rows shared over the batch."""
     H.need_gpu()
@@ -244,6 +246,28 @@ def test_decode_many_requests(B, Hq, Hkv, d, top, q4):
     c = Cache(rng, lens, 2, Hkv, d, q4)
     for _ in range(2):
         c.check(*c.step(rng, Hq))
+
+
+@pytest.mark.parametrize("q4", [True, False])
+def test_a_bound_far_above_the_lengths(q4):
+    """Most ranges of the grid have no rows; then shared rows with more workgroups than ranges."""
+    H.need_gpu()
+    rng = np.random.default_rng(21 + q4)
+    for lens, Hq, Hkv in (([3, 40, 0, 300], 4, 2), ([5] * 50, 8, 8)):
+        c = Cache(rng, lens, 2, Hkv, 64, q4)
+        for _ in range(2):
+            c.check(*c.step(rng, Hq, max_ctx=9000))
+
+
+def test_no_tokens_at_all():
+    H.need_gpu()
+    k = torch.zeros((0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    c = Q4Cache(4, 2, 64, np.array([0, 2]), np.array([2, 2]), "cuda")
+    c.length.fill_(9)
+    status = i32([0])
+    assert sonic.kv_compact_q4(i32([0, 0, 0]), torch.zeros(0, dtype=torch.uint8, device="cuda"), k, k, c.k, c.k_scale, c.v, c.v_scale, c.row_off,
+                               c.row_cap, c.length, c.keep_idx, status, 0) == sonic.OK
+    assert c.length.tolist() == [0, 0] and int(status.item()) == 0 and torch.all(c.k == 255)
 
 
 def test_decode_without_weights_gives_the_same_outputs():
