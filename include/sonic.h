@@ -335,7 +335,8 @@ size_t sonic_decode_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t 
  *   out            device fp32 [B][Hq][d]
  *   workspace      device, 256-byte aligned, >= sonic_decode_workspace_bytes(B, Hq, d,
  *                  max_ctx); zero-filled before its first use (it holds completion
- *                  counters that every call leaves at zero again)
+ *                  counters that every call leaves at zero again), and again before a
+ *                  call of another B or Hkv, on which the counters' places depend
  *   dev_status     SONIC_ERR_CAPACITY when cache_len[b] + 1 exceeds the capacity
  *                  or max_ctx: request b is then left unchanged (no append, no
  *                  output, same length) while the other requests proceed.
@@ -503,8 +504,8 @@ size_t sonic_decode_q4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32
  *   row_weight   NULL, or device fp32 [rows]: see sonic_compressed_decode_weighted
  * The other arguments, outputs and errors are those of sonic_compressed_decode without
  * row_role; a NaN row makes the outputs it reaches NaN.  The workspace is zero-filled before its
- * first use, and again before calls of another shape (batch, heads, head_dim, max_ctx); one made for
- * weights serves calls without them too.  Calls that share one must not run concurrently.
+ * first use, and again before a call of another B or Hkv; one made for weights, or for a longer max_ctx,
+ * serves calls without them, or shorter ones, too.  Calls that share one must not run concurrently.
  */
 int32_t sonic_compressed_decode_q4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                    int32_t max_ctx, void *k_cache, void *k_scale, void *v_cache, void *v_scale,
@@ -546,8 +547,8 @@ size_t sonic_decode_weighted_workspace_bytes(int32_t batch, int32_t num_q_heads,
  *                does not know of it: after it the caller sets the rows it wrote.
  * The other arguments, outputs and errors are those of sonic_compressed_decode without
  * row_role; the workspace (sonic_decode_weighted_workspace_bytes) is larger by the scores,
- * batch * num_q_heads * max_ctx floats, and zero-filled before its first use and before calls of
- * another shape.  Calls that share one must not run concurrently.
+ * batch * num_q_heads * max_ctx floats, and zero-filled before its first use and before a call of
+ * another B or Hkv.  Calls that share one must not run concurrently.
  */
 int32_t sonic_compressed_decode_weighted(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                          int32_t max_ctx, void *k_cache, void *v_cache, const int64_t *cache_row_off,
