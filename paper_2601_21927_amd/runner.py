@@ -7,6 +7,7 @@ stream; every step of the path runs in libsonic.so.
 """
 from __future__ import annotations
 
+import functools
 from typing import Optional, Sequence
 
 import numpy as np
@@ -97,6 +98,42 @@ class SonicBatch:
         self.status.zero_()
 
 
+class _Workspaces:
+    """Device workspaces of a cache's calls.
+
+    One is made on the stream of the call that first needs it, so that its zeros are in place for that call, and kept
+    as long as the cache: a larger one does not replace it for what is still running on a stream or was captured into a
+    graph.  Sizes double, so the smaller ones add up to no more than the last.
+    """
+
+    def __init__(self):
+        self.made = {}
+
+    def get(self, key, nbytes: int, device, stream, counters: int = 0) -> torch.Tensor:
+        """A workspace of nbytes or more for calls of one key (the numbers that its counters' places depend on);
+        `counters`: its bytes from the start on that have to be zero before the first call, which leaves them so."""
+        fits = [w for w in self.made.get(key, ()) if w.numel() >= nbytes]
+        if fits:
+            return fits[-1]
+        with torch.cuda.stream(stream):
+            mine = self.made.setdefault(key, [])
+            mine.append(torch.empty(max(nbytes, 256, 2 * mine[-1].numel() if mine else 0), dtype=torch.uint8, device=device))
+            ws = mine[-1]
+            ws[:counters].zero_()
+        return ws
+
+
+@functools.lru_cache(maxsize=1024)
+def _bytes(size, *shape) -> int:
+    return size(*shape)
+
+
+def _counter_bytes(batch: int, num_kv_heads: int) -> int:
+    """The completion counters' share of a decode workspace: int32 per request and per (request, kv-head), each array on
+    256 bytes."""
+    return sum((4 * n + 255) // 256 * 256 for n in (batch, batch * num_kv_heads))
+
+
 class CompactCache:
     """Per-request cache rows [row_off[b], row_off[b] + row_cap[b]) of a [rows, Hkv, d] bf16 pair."""
 
@@ -112,41 +149,32 @@ class CompactCache:
         self.row_cap = torch.from_numpy(self.row_cap_host).to(device)
         self.length = torch.zeros(len(row_cap), dtype=torch.int32, device=device)
         self.batch = len(row_cap)
-        self.ws = None
-        self.ws_key = None
+        self.workspaces = _Workspaces()
         self.row_weight = None
-        self.weighted_ws = None
-        self.weighted_ws_key = None
 
     def decode(self, q, k_new, v_new, out, status, max_ctx: int, row_role: Optional[torch.Tensor] = None,
                stream=None) -> int:
-        B, Hq, d = q.shape
-        Hkv = k_new.shape[1]
-        key = (B, Hq, Hkv, d, int(max_ctx))
-        if self.ws_key != key:
-            n = sonic.decode_workspace_bytes(B, Hq, d, int(max_ctx))
-            self.ws = torch.zeros(max(n, 256), dtype=torch.uint8, device=q.device)   # counters start at zero
-            self.ws_key = key
+        ws = self._decode_ws(_bytes(sonic.decode_workspace_bytes, *q.shape, int(max_ctx)), k_new, stream)
         return sonic.compressed_decode(self.k, self.v, self.row_off, self.row_cap, self.length, q, k_new, v_new,
-                                       out, self.ws, status, max_ctx, row_role=row_role, stream=stream)
+                                       out, ws, status, max_ctx, row_role=row_role, stream=stream)
+
+    def _decode_ws(self, nbytes, k_new, stream):
+        B, Hkv = k_new.shape[:2]
+        return self.workspaces.get(("decode", B, Hkv), nbytes, k_new.device, stream, _counter_bytes(B, Hkv))
 
     def decode_weighted(self, q, k_new, v_new, out, status, max_ctx: int, stream=None) -> int:
         """decode that also adds each row's attention to row_weight."""
-        B, Hq, d = q.shape
-        key = (B, Hq, d, int(max_ctx))
         if self.row_weight is None:
-            self.row_weight = torch.zeros(self.k.shape[0], dtype=torch.float32, device=q.device)
-        if self.weighted_ws_key != key:
-            n = sonic.decode_weighted_workspace_bytes(B, Hq, d, int(max_ctx))
-            self.weighted_ws = torch.zeros(n, dtype=torch.uint8, device=q.device)   # counters start at zero
-            self.weighted_ws_key = key
+            with torch.cuda.stream(stream):
+                self.row_weight = torch.zeros(self.k.shape[0], dtype=torch.float32, device=q.device)
+        ws = self._decode_ws(_bytes(sonic.decode_weighted_workspace_bytes, *q.shape, int(max_ctx)), k_new, stream)
         return sonic.compressed_decode_weighted(self.k, self.v, self.row_off, self.row_cap, self.length, q, k_new, v_new, out,
-                                                self.row_weight, self.weighted_ws, status, max_ctx, stream=stream)
+                                                self.row_weight, ws, status, max_ctx, stream=stream)
 
     def evict(self, keep_head, keep_tail, budget, status, stream=None) -> int:
         """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device."""
         n = int(self.row_cap_host.max()) if self.batch else 0
-        ws = torch.empty(sonic.cache_evict_workspace_bytes(self.batch, n), dtype=torch.uint8, device=self.k.device)
+        ws = self.workspaces.get("evict", sonic.cache_evict_workspace_bytes(self.batch, n), self.k.device, stream)
         return sonic.cache_evict(self.k, self.v, self.row_off, self.length, self.row_weight, keep_head, keep_tail, budget, ws,
                                  status, n, stream=stream)
 
@@ -170,18 +198,14 @@ class Q4Cache:
         self.row_cap = torch.from_numpy(self.row_cap_host).to(device)
         self.length = torch.zeros(len(row_cap), dtype=torch.int32, device=device)
         self.batch = len(row_cap)
-        self.ws = None
-        self.ws_key = None
+        self.workspaces = _Workspaces()
 
     def decode(self, q, k_new, v_new, out, status, max_ctx: int, weighted: bool = False, stream=None) -> int:
-        B, Hq, d = q.shape
-        key = (B, Hq, d, int(max_ctx), weighted)
-        if self.ws_key != key:
-            n = sonic.decode_q4_workspace_bytes(B, Hq, d, int(max_ctx), weighted)
-            self.ws = torch.zeros(n, dtype=torch.uint8, device=q.device)   # counters start at zero
-            self.ws_key = key
+        B, Hkv = k_new.shape[:2]
+        n = _bytes(sonic.decode_q4_workspace_bytes, *q.shape, int(max_ctx), weighted)
+        ws = self.workspaces.get(("decode", B, Hkv), n, q.device, stream, _counter_bytes(B, Hkv))
         return sonic.compressed_decode_q4(self.k, self.k_scale, self.v, self.v_scale, self.row_off, self.row_cap, self.length, q,
-                                          k_new, v_new, out, self.ws, status, max_ctx,
+                                          k_new, v_new, out, ws, status, max_ctx,
                                           row_weight=self.row_weight if weighted else None, stream=stream)
 
     def expand(self, row_begin, row_end, k, v, out_row_off, out_row_cap, status, max_rows: int, stream=None) -> int:
@@ -191,6 +215,6 @@ class Q4Cache:
     def evict(self, keep_head, keep_tail, budget, status, stream=None) -> int:
         """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device."""
         n = int(self.row_cap_host.max()) if self.batch else 0
-        ws = torch.empty(sonic.cache_evict_workspace_bytes(self.batch, n), dtype=torch.uint8, device=self.k.device)
+        ws = self.workspaces.get("evict", sonic.cache_evict_workspace_bytes(self.batch, n), self.k.device, stream)
         return sonic.cache_evict(self.k, self.v, self.row_off, self.length, self.row_weight, keep_head, keep_tail, budget, ws,
                                  status, n, k_scale=self.k_scale, v_scale=self.v_scale, stream=stream)

@@ -1,0 +1,70 @@
+"""The cache classes on other streams than the current one, and under capture."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import evict as OE
+from paper_2601_21927_amd import sonic
+from paper_2601_21927_amd.runner import bf16_to_device
+from tests import gpu_helpers as H
+from tests.test_gpu_q4 import Cache, i32, normal_bits
+
+pytestmark = pytest.mark.gpu
+
+BUSY = 20_000_000   # cycles of a waiting kernel, some ten milliseconds
+
+
+@pytest.mark.parametrize("q4", [True, False])
+def test_eviction_on_another_stream_while_the_current_one_allocates(q4):
+    H.need_gpu()
+    rng = np.random.default_rng(31 + q4)
+    c = Cache(rng, [700, 30, 3000, 90], 2, 2, 128, q4)
+    want = [OE.kept_rows(c.weight[o:o + n], 8, 5, 100) for o, n in zip(c.off, c.lens)]
+    before = [x.clone() for x in (c.dev.k, c.dev.v, c.dev.row_weight)]
+    lim = [i32([x] * 4) for x in (8, 5, 100)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+    assert c.dev.evict(*lim, c.status, stream=side) == sonic.OK
+    size = sonic.cache_evict_workspace_bytes(4, int(c.cap.max()))
+    held = [torch.full((size,), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(20)]
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == 0 and all(int(x[0]) == 0x7F for x in held)
+    assert c.dev.length.tolist() == [len(w) for w in want]
+    for old, x in zip(before, (c.dev.k, c.dev.v, c.dev.row_weight)):
+        for o, kept in zip(c.off, want):
+            assert torch.equal(x[o:o + len(kept)], old[o + torch.from_numpy(kept).cuda()])
+
+
+@pytest.mark.parametrize("q4,weighted", [(True, True), (True, False), (False, True), (False, False)])
+def test_a_first_step_on_another_stream_while_the_current_one_is_busy(q4, weighted):
+    """The workspace's zeros are written where the step waits for them, and a replaced workspace is not handed out."""
+    H.need_gpu()
+    rng = np.random.default_rng(33 + q4)
+    c = Cache(rng, [700, 30, 3000], 4, 2, 64, q4)
+    side = torch.cuda.Stream()
+    dirt = [torch.full((1 << 22,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    del dirt          # what the allocator hands out next is not zero
+    torch.cuda.synchronize()
+    torch.cuda._sleep(BUSY)
+    for bound in (c.max_ctx, 9000):
+        q, k, v = (normal_bits(rng, 3, h, 64) for h in (8, 2, 2))
+        with torch.cuda.stream(side):
+            args = [bf16_to_device(x) for x in (q, k, v)] + [torch.zeros((3, 8, 64), device="cuda"), c.status, bound]
+        if q4:
+            st = c.dev.decode(*args, weighted=weighted, stream=side)
+        else:
+            st = (c.dev.decode_weighted if weighted else c.dev.decode)(*args, stream=side)
+        assert st == sonic.OK
+        held = [torch.full((1 << 20,), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        side.synchronize()
+        with torch.cuda.stream(side):
+            if q4 or weighted:
+                c.check(q, k, v, args[3].cpu().numpy(), weighted=weighted)
+            else:
+                for b in range(3):
+                    H.assert_close(args[3][b].cpu().numpy(), c.expect(b, q, k, v)[0], f"request {b}")
+                    c.lens[b] += 1
+        del held
+    torch.cuda.synchronize()
