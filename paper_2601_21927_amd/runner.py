@@ -116,9 +116,14 @@ class _Workspaces:
         if fits:
             return fits[-1]
         with torch.cuda.stream(stream):
-            mine = self.made.setdefault(key, [])
-            mine.append(torch.empty(max(nbytes, 256, 2 * mine[-1].numel() if mine else 0), dtype=torch.uint8, device=device))
-            ws = mine[-1]
+            # zeros written under capture are there only when that graph runs: such a workspace is for captured calls,
+            # each of which clears the counters itself
+            if counters and torch.device(device).type == "cuda" and torch.cuda.is_current_stream_capturing():
+                ws = self.get((key, "captured"), nbytes, device, stream)
+            else:
+                mine = self.made.setdefault(key, [])
+                mine.append(torch.empty(max(nbytes, 256, 2 * mine[-1].numel() if mine else 0), dtype=torch.uint8, device=device))
+                ws = mine[-1]
             ws[:counters].zero_()
         return ws
 
@@ -166,6 +171,8 @@ class CompactCache:
         """decode that also adds each row's attention to row_weight."""
         if self.row_weight is None:
             with torch.cuda.stream(stream):
+                if q.is_cuda and torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("set row_weight before capturing: zeros made here would be written again by every replay")
                 self.row_weight = torch.zeros(self.k.shape[0], dtype=torch.float32, device=q.device)
         ws = self._decode_ws(_bytes(sonic.decode_weighted_workspace_bytes, *q.shape, int(max_ctx)), k_new, stream)
         return sonic.compressed_decode_weighted(self.k, self.v, self.row_off, self.row_cap, self.length, q, k_new, v_new, out,

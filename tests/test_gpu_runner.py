@@ -68,3 +68,66 @@ def test_a_first_step_on_another_stream_while_the_current_one_is_busy(q4, weight
                     c.lens[b] += 1
         del held
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("q4", [True, False])
+def test_a_step_captured_before_any_eager_one(q4):
+    """What a capture makes is not taken for zeroed by eager steps, nor by another graph."""
+    H.need_gpu()
+    rng = np.random.default_rng(35 + q4)
+    c = Cache(rng, [700, 30, 3000], 40, 2, 64, q4)
+    q, k, v = (bf16_to_device(normal_bits(rng, 3, h, 64)) for h in (8, 2, 2))
+    out, start, w0 = torch.zeros((3, 8, 64), device="cuda"), c.dev.length.clone(), c.dev.row_weight.clone()
+
+    def steps():
+        torch.add(start, 0, out=c.dev.length)
+        torch.add(w0, 0, out=c.dev.row_weight)
+        for _ in range(2):
+            args = (q, k, v, out, c.status, c.max_ctx)
+            assert (c.dev.decode(*args, weighted=True) if q4 else c.dev.decode_weighted(*args)) == sonic.OK
+
+    def result():
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (out, c.dev.row_weight, c.dev.length)]
+        out.zero_()
+        return got
+
+    dirt = [torch.full((1 << 22,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    del dirt
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for g in graphs:
+        with torch.cuda.graph(g):
+            steps()
+    steps()
+    want = result()
+    assert want[2].tolist() == [702, 32, 3002] and torch.isfinite(want[0]).all() and want[0].any()
+    for g in graphs[::-1] * 2:
+        g.replay()
+        assert all(torch.equal(x, y) for x, y in zip(result(), want))
+        steps()
+        assert all(torch.equal(x, y) for x, y in zip(result(), want))
+
+
+def test_weights_are_not_made_under_capture():
+    H.need_gpu()
+    rng = np.random.default_rng(37)
+    c = Cache(rng, [20, 30], 4, 2, 64, False)
+    q, k, v = (bf16_to_device(normal_bits(rng, 2, h, 64)) for h in (8, 2, 2))
+    out = torch.zeros((2, 8, 64), device="cuda")
+    c.dev.row_weight = None
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        g = torch.cuda.CUDAGraph()
+        g.capture_begin()
+        try:
+            with pytest.raises(RuntimeError, match="row_weight"):
+                c.dev.decode_weighted(q, k, v, out, c.status, c.max_ctx)
+            out.add_(1.0)
+        finally:
+            g.capture_end()
+    torch.cuda.synchronize()
+    assert c.dev.row_weight is None
+    assert c.dev.decode_weighted(q, k, v, out, c.status, c.max_ctx) == sonic.OK
+    assert c.dev.length.tolist() == [21, 31] and bool((c.dev.row_weight > 0).any())
