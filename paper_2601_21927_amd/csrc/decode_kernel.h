@@ -472,7 +472,9 @@ __global__ __launch_bounds__(NW * kWave, Q4 ? 4 : 2) void decode_kernel(
   f32x4 oacc[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) oacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = -INFINITY;   // running max (log2 domain) of column col, lagging by at most 8
+  // Running max (log2 domain) of column col, lagging by at most 8.  4-bit rows start at the lowest number: a block
+  // whose scores all passed the range below (-infinity) then weighs exp2(-infinity), 0, without a test in the loop.
+  float m_run = Q4 ? -__FLT_MAX__ : -INFINITY;
   float l_run = 0.f;         // this lane's share of the column's sum
 
   // transposed-read geometry (value product): 16-lane group kq reads rows 4*kq + (t >> 2)
@@ -807,13 +809,13 @@ __global__ __launch_bounds__(NW * kWave, Q4 ? 4 : 2) void decode_kernel(
       mloc = pair32_max(pair16_max(mloc)) * scale_log2;
       if (__any(mloc > m_run + 8.f)) {   // rescale only when the max grows by more than 2^8
         const float m_new = fmaxf(m_run, mloc);
-        const float corr = (m_run == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
         l_run *= corr;
 #pragma unroll
         for (int i = 0; i < DB; ++i) oacc[i] *= corr;
       }
-      f32x8 p;   // (a masked score is -infinity, and every block has a row that is not)
+      f32x8 p;   // (a masked score is -infinity)
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], scale_log2, -m_run));
       auto rounded = [](const f32x8 &x) { return __builtin_convertvector(__builtin_convertvector(x, bf16x8), f32x8); };
