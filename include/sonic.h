@@ -486,7 +486,7 @@ int32_t sonic_kv_compact_q4(int32_t batch, int32_t total_tokens, int32_t max_seq
  *   out_row_cap           device int32 [B]: output rows request b owns
  *   dev_status            SONIC_ERR_BAD_LAYOUT for a bad range, SONIC_ERR_CAPACITY for more rows
  *                         than out_row_cap[b], SONIC_ERR_INVALID_ARG for more than max_rows;
- *                         nothing is written for that request
+ *                         nothing is written for that request, and the others are expanded
  */
 int32_t sonic_cache_expand_q4(int32_t batch, int32_t max_rows, int32_t num_kv_heads, int32_t head_dim,
                               const void *k_cache, const void *k_scale, const void *v_cache, const void *v_scale,

@@ -11,25 +11,38 @@ namespace sonic {
 constexpr int kRowThreads = 256;
 constexpr int kExpandUnroll = 4;
 
+// What is wrong with request b's range, or 0.
+__device__ __forceinline__ int range_error(int r0, int r1, int cap, int room, int max_rows) {
+  if (r0 < 0 || r1 < r0 || r1 > cap) return SONIC_ERR_BAD_LAYOUT;
+  return r1 - r0 > room ? SONIC_ERR_CAPACITY : r1 - r0 > max_rows ? SONIC_ERR_INVALID_ARG : 0;
+}
+
+// Errors are raised by a kernel of their own, behind the one that writes: a workgroup that starts late takes a status word
+// for one that was pending before the call, and would leave out its rows when another request's error is already in it.
+__global__ __launch_bounds__(kRowThreads) void expand_errors_kernel(const int32_t *__restrict__ row_begin,
+                                                                    const int32_t *__restrict__ row_end,
+                                                                    const int32_t *__restrict__ row_cap,
+                                                                    const int32_t *__restrict__ out_cap, int batch, int max_rows,
+                                                                    int32_t *status) {
+  const int b = blockIdx.x * kRowThreads + threadIdx.x;
+  if (b >= batch) return;
+  const int code = range_error(row_begin[b], row_end[b], row_cap[b], out_cap[b], max_rows);
+  if (code != 0) raise_status(status, code);
+}
+
 // Request b's rows row_begin[b] .. row_end[b] to rows out_off[b] .. of k and v.  Grid (chunks of units, requests);
 // a unit is eight values, four bytes of codes in and sixteen out, so that loads and stores are both whole lines.
 __global__ __launch_bounds__(kRowThreads) void expand_q4_kernel(
     const uint32_t *__restrict__ kc, const uint8_t *__restrict__ kscale, const uint32_t *__restrict__ vc,
     const uint8_t *__restrict__ vscale, const int64_t *__restrict__ row_off, const int32_t *__restrict__ row_cap,
     const int32_t *__restrict__ row_begin, const int32_t *__restrict__ row_end, bf16x8 *__restrict__ k, bf16x8 *__restrict__ v,
-    const int64_t *__restrict__ out_off, const int32_t *__restrict__ out_cap, int max_rows, int row_units, int32_t *status) {
+    const int64_t *__restrict__ out_off, const int32_t *__restrict__ out_cap, int max_rows, int row_units, const int32_t *status) {
   __shared__ int s_ok;
   const int b = blockIdx.y;
   const int r0 = row_begin[b], r1 = row_end[b], cap = row_cap[b], room = out_cap[b];
   const int64_t off = row_off[b], out0 = out_off[b];
   if (!block_status_clear(status, &s_ok)) return;
-  if (r0 < 0 || r1 < r0 || r1 > cap || r1 - r0 > room || r1 - r0 > max_rows) {
-    if (blockIdx.x == 0 && threadIdx.x == 0)
-      raise_status(status, r0 < 0 || r1 < r0 || r1 > cap ? SONIC_ERR_BAD_LAYOUT
-                           : r1 - r0 > room              ? SONIC_ERR_CAPACITY
-                                                         : SONIC_ERR_INVALID_ARG);
-    return;
-  }
+  if (range_error(r0, r1, cap, room, max_rows) != 0) return;
   const long total = static_cast<long>(r1 - r0) * row_units;
   const size_t src0 = static_cast<size_t>(off + r0) * row_units, dst0 = static_cast<size_t>(out0) * row_units;
   const long step = static_cast<long>(gridDim.x) * kRowThreads;
@@ -143,6 +156,10 @@ hipError_t launch_expand_q4(int batch, int max_rows, int Hkv, int D, const uint8
   expand_q4_kernel<<<dim3(chunks, batch), dim3(kRowThreads), 0, stream>>>(
       reinterpret_cast<const uint32_t *>(kc), ks, reinterpret_cast<const uint32_t *>(vc), vs, row_off, row_cap, row_begin, row_end,
       reinterpret_cast<bf16x8 *>(k), reinterpret_cast<bf16x8 *>(v), out_off, out_cap, max_rows, row_units, status);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  expand_errors_kernel<<<dim3((batch + kRowThreads - 1) / kRowThreads), dim3(kRowThreads), 0, stream>>>(row_begin, row_end, row_cap,
+                                                                                                        out_cap, batch, max_rows, status);
   return hipGetLastError();
 }
 
