@@ -527,7 +527,8 @@ int32_t sonic_compressed_decode_q4(int32_t batch, int32_t num_q_heads, int32_t n
  *   key_weight    device fp32 [T] (sonic_segment_attn_prefill);  row_weight: device fp32 [rows]
  *   dev_status    SONIC_ERR_BAD_LAYOUT for inconsistent cu_seqlens, a negative length, or a
  *                 keep_idx outside its request (the row keeps its weight),
- *                 SONIC_ERR_INVALID_ARG for more rows than max_rows
+ *                 SONIC_ERR_INVALID_ARG for more rows than max_rows (the request's rows keep theirs,
+ *                 as with inconsistent cu_seqlens or a negative length); all other rows are written
  */
 int32_t sonic_kv_compact_weights(int32_t batch, int32_t total_tokens, int32_t max_rows, const int32_t *cu_seqlens,
                                  const float *key_weight, const int64_t *cache_row_off, const int32_t *cache_len,

@@ -69,7 +69,9 @@ __global__ __launch_bounds__(kRowThreads) void expand_q4_kernel(
   }
 }
 
-// row_weight of request b's row j = the key weight of the prompt position keep_idx holds for it.
+// row_weight of request b's row j = the key weight of the prompt position keep_idx holds for it.  ERRORS: raises what is
+// wrong, behind the launch that writes (see expand_errors_kernel).
+template <bool ERRORS>
 __global__ __launch_bounds__(kRowThreads) void compact_weights_kernel(
     const int32_t *__restrict__ cu, const float *__restrict__ key_weight, const int64_t *__restrict__ row_off,
     const int32_t *__restrict__ cache_len, const int32_t *__restrict__ keep_idx, float *__restrict__ row_weight,
@@ -80,15 +82,19 @@ __global__ __launch_bounds__(kRowThreads) void compact_weights_kernel(
   const int64_t off = row_off[b];
   if (!block_status_clear(status, &s_ok)) return;
   if (s < 0 || e < s || e > total_tokens || len < 0 || len > max_rows) {
-    if (blockIdx.x == 0 && threadIdx.x == 0)
+    if (ERRORS && blockIdx.x == 0 && threadIdx.x == 0)
       raise_status(status, len > max_rows ? SONIC_ERR_INVALID_ARG : SONIC_ERR_BAD_LAYOUT);
     return;
   }
   const int j = blockIdx.x * kRowThreads + threadIdx.x;
   if (j >= len) return;
   const int p = keep_idx[off + j];
-  if (p < 0 || p >= e - s) raise_status(status, SONIC_ERR_BAD_LAYOUT);
-  else row_weight[off + j] = key_weight[s + p];
+  const bool in = p >= 0 && p < e - s;
+  if (ERRORS) {
+    if (!in) raise_status(status, SONIC_ERR_BAD_LAYOUT);
+  } else if (in) {
+    row_weight[off + j] = key_weight[s + p];
+  }
 }
 
 // After a decode step that kept its scores: row r's weight grows by the mean over the q-heads of
@@ -166,8 +172,13 @@ hipError_t launch_expand_q4(int batch, int max_rows, int Hkv, int D, const uint8
 hipError_t launch_compact_weights(int batch, int total_tokens, int max_rows, const int32_t *cu, const float *key_weight,
                                   const int64_t *row_off, const int32_t *cache_len, const int32_t *keep_idx, float *row_weight,
                                   int32_t *status, hipStream_t stream) {
-  compact_weights_kernel<<<dim3(std::max(1, (max_rows + kRowThreads - 1) / kRowThreads), batch), dim3(kRowThreads), 0, stream>>>(
-      cu, key_weight, row_off, cache_len, keep_idx, row_weight, total_tokens, max_rows, status);
+  const dim3 grid(std::max(1, (max_rows + kRowThreads - 1) / kRowThreads), batch);
+  compact_weights_kernel<false><<<grid, dim3(kRowThreads), 0, stream>>>(cu, key_weight, row_off, cache_len, keep_idx, row_weight,
+                                                                        total_tokens, max_rows, status);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  compact_weights_kernel<true><<<grid, dim3(kRowThreads), 0, stream>>>(cu, key_weight, row_off, cache_len, keep_idx, row_weight,
+                                                                       total_tokens, max_rows, status);
   return hipGetLastError();
 }
 

@@ -39,3 +39,37 @@ def test_expansion_writes_every_request_but_the_one_at_fault(at, begin, end, cap
     for x in (k, v):
         assert bool((x[others, :n] == 1.0).all()) and bool((x[others, n:] == 5.0).all())
         assert bool((x[at] == 5.0).all())
+
+
+def weights_call(c, key_weight, cu, status, max_rows=ROWS):
+    return sonic.kv_compact_weights(cu, key_weight, c.row_off, c.length, c.keep_idx, c.row_weight, status, max_rows)
+
+
+@pytest.mark.parametrize("fault,code", [("index", sonic.ERR_BAD_LAYOUT), ("negative index", sonic.ERR_BAD_LAYOUT), ("length", sonic.ERR_INVALID_ARG),
+                                        ("negative length", sonic.ERR_BAD_LAYOUT)])
+@pytest.mark.parametrize("at", [0, B - 1])
+def test_key_weights_reach_every_row_but_those_at_fault(at, fault, code):
+    H.need_gpu()
+    cap = ROWS + 1
+    c = Q4Cache(B * cap, 1, 64, np.arange(B, dtype=np.int64) * cap, np.full(B, cap), "cuda")
+    c.length.fill_(ROWS)
+    c.keep_idx.copy_(torch.arange(B * cap, device="cuda") % cap)
+    c.row_weight.fill_(-1.0)
+    key_weight = torch.rand(B * ROWS, device="cuda")
+    cu = i32(np.arange(B + 1) * ROWS)
+    want = torch.full((B, cap), -1.0, device="cuda")
+    want[:, :ROWS] = key_weight.view(B, ROWS)
+    if "index" in fault:
+        c.keep_idx[at * cap + 7] = ROWS if fault == "index" else -1
+        want[at, 7] = -1.0
+    else:
+        c.length[at] = ROWS + 1 if fault == "length" else -1
+        want[at] = -1.0
+    status = i32([0])
+    assert weights_call(c, key_weight, cu, status) == sonic.OK
+    assert int(status.item()) == code
+    assert torch.equal(c.row_weight.view(B, cap), want)
+    # a status that was pending before the call stops it
+    c.row_weight.fill_(-1.0)
+    assert weights_call(c, key_weight, cu, status) == sonic.OK
+    assert int(status.item()) == code and bool((c.row_weight == -1.0).all())
