@@ -259,7 +259,7 @@ struct EvictCall {
 // Workspace of an eviction.
 struct EvictWs {
   int32_t *ctrl;     // [0]: the call is to be done
-  int2 *req;         // [B] rows kept, rows before the first dropped one
+  int2 *req;         // [B] rows kept (below 0: the request is left as it is), rows before the first dropped one
   int32_t *list;     // [B][max_rows] the kept rows in order
 };
 

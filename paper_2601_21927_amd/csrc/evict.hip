@@ -86,8 +86,15 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, Evi
   __shared__ int s_ok, s_first;
   __shared__ Digit s_digit;
   const int b = blockIdx.x;
-  // workgroup 0's look at the status word decides for the whole call
-  const bool clear = b != 0 || block_status_clear(c.status, &s_ok);
+  // Behind a pending error a length may be anything: no weight is read for it.  Workgroup 0's look decides for the call;
+  // a request whose workgroup saw an error that workgroup 0 did not (the word may change meanwhile) is left as it is.
+  if (!block_status_clear(c.status, &s_ok)) {
+    if (threadIdx.x == 0) {
+      if (b == 0) ws.ctrl[0] = 0;
+      ws.req[b] = make_int2(-1, 0);
+    }
+    return;
+  }
   EvictReq own;
   const int own_code = evict_check(b, c, &own);
   const float *w = c.row_weight + c.row_off[b];
@@ -119,8 +126,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, Evi
   if (threadIdx.x == 0) s_first = own.kept;
   bad = __syncthreads_or(bad);
   if (own_code != 0 && threadIdx.x == 0) raise_status(c.status, own_code);
-  if (b == 0 && threadIdx.x == 0) ws.ctrl[0] = clear && !bad;
-  if (bad || !clear) return;
+  if (b == 0 && threadIdx.x == 0) ws.ctrl[0] = !bad;
+  if (bad) return;
 
   int32_t *list = ws.list + static_cast<size_t>(b) * c.max_rows;
   const int take = own.kept - own.head - own.tail;   // of the middle rows
@@ -215,6 +222,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictCall c, EvictWs
   if (ws.ctrl[0] == 0) return;
   const int b = blockIdx.y;
   const int kept = ws.req[b].x;
+  if (kept < 0) return;
   const int32_t *list = ws.list + static_cast<size_t>(b) * c.max_rows;
   const size_t src0 = c.row_off[b], dst0 = c.out_row_off[b];
   const long first = static_cast<long>(blockIdx.x) * kMoveThreads + threadIdx.x, step = static_cast<long>(gridDim.x) * kMoveThreads;
@@ -300,6 +308,7 @@ __global__ __launch_bounds__(kWalkThreads) void move_in_place_kernel(EvictCall c
   if (ws.ctrl[0] == 0) return;
   const int b = blockIdx.y;
   const int kept = ws.req[b].x, first = ws.req[b].y;
+  if (kept < 0) return;
   const int32_t *list = ws.list + static_cast<size_t>(b) * c.max_rows;
   const size_t row0 = c.row_off[b];
   const int cols = (row_units + col_units - 1) / col_units;
