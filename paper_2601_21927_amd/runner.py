@@ -139,6 +139,28 @@ def _counter_bytes(batch: int, num_kv_heads: int) -> int:
     return sum((4 * n + 255) // 256 * 256 for n in (batch, batch * num_kv_heads))
 
 
+def _places(rows, row_off, row_cap, device):
+    """Of every cache row, on the device: the first row of the request that owns it (int64), and its place in it (int32)."""
+    first, place = np.zeros(rows, np.int64), np.arange(rows, dtype=np.int32)
+    for o, n in zip(row_off, row_cap):
+        place[o:o + n] -= place[o:o + 1]
+        first[o:o + n] = o
+    return torch.from_numpy(first).to(device), torch.from_numpy(place).to(device)
+
+
+def _evict(cache, keep_head, keep_tail, budget, status, stream, **scales) -> int:
+    """sonic.cache_evict in place; keep_idx moves with the rows, so that each still names its prompt position."""
+    n = int(cache.row_cap_host.max()) if cache.batch else 0
+    ws = cache.workspaces.get("evict", sonic.cache_evict_workspace_bytes(cache.batch, n), cache.k.device, stream)
+    with torch.cuda.stream(stream):
+        moved = cache.place.clone()   # where nothing moves: each row's own
+        st = sonic.cache_evict(cache.k, cache.v, cache.row_off, cache.length, cache.row_weight, keep_head, keep_tail, budget, ws,
+                               status, n, keep_idx=moved, stream=stream, **scales)
+        if st == sonic.OK:
+            cache.keep_idx.copy_(cache.keep_idx[(cache.first_row + moved).clamp_(max=moved.numel() - 1)])
+    return st
+
+
 class CompactCache:
     """Per-request cache rows [row_off[b], row_off[b] + row_cap[b]) of a [rows, Hkv, d] bf16 pair."""
 
@@ -154,6 +176,7 @@ class CompactCache:
         self.row_cap = torch.from_numpy(self.row_cap_host).to(device)
         self.length = torch.zeros(len(row_cap), dtype=torch.int32, device=device)
         self.batch = len(row_cap)
+        self.first_row, self.place = _places(self.keep_idx.numel(), self.row_off_host, self.row_cap_host, device)
         self.workspaces = _Workspaces()
         self.row_weight = None
 
@@ -179,11 +202,9 @@ class CompactCache:
                                                 self.row_weight, ws, status, max_ctx, stream=stream)
 
     def evict(self, keep_head, keep_tail, budget, status, stream=None) -> int:
-        """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device."""
-        n = int(self.row_cap_host.max()) if self.batch else 0
-        ws = self.workspaces.get("evict", sonic.cache_evict_workspace_bytes(self.batch, n), self.k.device, stream)
-        return sonic.cache_evict(self.k, self.v, self.row_off, self.length, self.row_weight, keep_head, keep_tail, budget, ws,
-                                 status, n, stream=stream)
+        """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device.  keep_idx
+        goes with the rows."""
+        return _evict(self, keep_head, keep_tail, budget, status, stream)
 
 
 class Q4Cache:
@@ -205,6 +226,7 @@ class Q4Cache:
         self.row_cap = torch.from_numpy(self.row_cap_host).to(device)
         self.length = torch.zeros(len(row_cap), dtype=torch.int32, device=device)
         self.batch = len(row_cap)
+        self.first_row, self.place = _places(self.keep_idx.numel(), self.row_off_host, self.row_cap_host, device)
         self.workspaces = _Workspaces()
 
     def decode(self, q, k_new, v_new, out, status, max_ctx: int, weighted: bool = False, stream=None) -> int:
@@ -220,8 +242,6 @@ class Q4Cache:
                                      v, out_row_off, out_row_cap, status, max_rows, stream=stream)
 
     def evict(self, keep_head, keep_tail, budget, status, stream=None) -> int:
-        """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device."""
-        n = int(self.row_cap_host.max()) if self.batch else 0
-        ws = self.workspaces.get("evict", sonic.cache_evict_workspace_bytes(self.batch, n), self.k.device, stream)
-        return sonic.cache_evict(self.k, self.v, self.row_off, self.length, self.row_weight, keep_head, keep_tail, budget, ws,
-                                 status, n, k_scale=self.k_scale, v_scale=self.v_scale, stream=stream)
+        """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device.  keep_idx
+        goes with the rows."""
+        return _evict(self, keep_head, keep_tail, budget, status, stream, k_scale=self.k_scale, v_scale=self.v_scale)
