@@ -783,7 +783,8 @@ int32_t sonic_kv_compact_q4(int32_t batch, int32_t total_tokens, int32_t max_seq
   const int32_t st = check_compact(batch, total_tokens, max_seqlen, Hkv, d, cu_seqlens, role, k, v, k_cache, v_cache, cache_row_off,
                                    cache_row_cap, cache_len, keep_idx, dev_status, &empty);
   if (st != SONIC_OK || empty) return st;
-  if (!k_scale || !v_scale || !aligned(k_scale, 4) || !aligned(v_scale, 4)) return SONIC_ERR_INVALID_ARG;
+  if (!aligned(k_scale, 4) || !aligned(v_scale, 4)) return SONIC_ERR_INVALID_ARG;
+  if (total_tokens > 0 && (!k_scale || !v_scale)) return SONIC_ERR_INVALID_ARG;   // (without tokens either form writes lengths only)
   const hipError_t e = launch_compact(batch, total_tokens, max_seqlen, Hkv, d, cu_seqlens, role, static_cast<const uint16_t *>(k),
                                       static_cast<const uint16_t *>(v), static_cast<uint16_t *>(k_cache),
                                       static_cast<uint16_t *>(v_cache), static_cast<uint8_t *>(k_scale),
