@@ -128,3 +128,26 @@ def test_probabilities_go_in_whole(Hq, Hkv, d, q4, weighted):
         for wrong in seen:
             seen[wrong] = max(seen[wrong], np.abs(np.tile(planted(c, b, q, wrong), d // 4) - want).max())
     assert all(x > 25 * U for x in seen.values()), seen     # the bar tells these mistakes
+
+
+@pytest.mark.parametrize("q4", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 2, 64), (16, 2, 128)])
+def test_weights_of_large_scores(Hq, Hkv, d, q4):
+    """Scores of several hundred.  With S the largest sum of |q k| over a row, scaled, in log2 units: a score is off by
+    2 d U S (an addition for each product) and 3 U S for the scale, the normaliser by as much and by 2 U for each
+    row of its sum and 16 U for the probabilities' own errors, their difference by 2 U S; then the exponential and the mean
+    as above."""
+    H.need_gpu()
+    rng = np.random.default_rng(71 + q4 + d)
+    c = Cache(rng, [500, 3, 47], 2, Hkv, d, q4)
+    q, k, v, out = c.step(rng, Hq, scale=50.0)
+    got = c.dev.row_weight.cpu().numpy()
+    for b in range(3):
+        o, n = int(c.off[b]), int(c.lens[b])
+        _, w = c.expect(b, q, k, v)
+        keys = np.abs(c.values[0][o:o + n + 1])
+        S = max((keys[:, h * Hkv // Hq] @ np.abs(bf16_bits_to_f64(q[b, h]))).max() for h in range(Hq)) * np.log2(np.e) / np.sqrt(d)
+        rel = np.exp2((2 * (2 * d + 3) + 2) * U * S + (2 * n + 16) * U) - 1 + (18 + Hq) * U
+        assert rel < 0.1
+        full = w + np.concatenate([c.weight[o:o + n].astype(np.float64), [0.0]])
+        assert np.all(np.abs(got[o:o + n + 1] - full) <= rel * w + U * full + 2.0 ** -126), b
