@@ -453,9 +453,11 @@ int32_t sonic_nexus_extend(int32_t batch, int32_t total_new, int32_t num_q_heads
  * stands for that number times 2^(scale - 127).  A block of largest magnitude a gets
  * the smallest e in [-127, 125] with a <= 7 * 2^e (125 if there is none), scale e + 127, and every value x of it
  * the nearest number to x / 2^e (ties to the even index; above 6, 6).  So a value is off
- * by at most max(2^e / 4, |x| / 5), 2^e being between a / 7 and 2 a / 7; rows rounded once
- * and expanded round to the same codes again; and the rows take d/2 + d/32 bytes per
- * head, 0.27 of bf16.  A block that holds an infinity or a NaN has scale 255 and is NaN
+ * by at most max(2^e / 4, |x| / 5), 2^e being between a / 7 and 2 a / 7 unless e is -127
+ * (a below 7 * 2^-128; a value is then off by 2^-129 or |x| / 5) or a is above 7 * 2^125
+ * (2.98e38; e is 125 and values above that become 6 * 2^125, off by less than |x| / 4); rows
+ * rounded once and expanded round to the same codes again; and the rows take d/2 + d/32
+ * bytes per head, 0.27 of bf16.  A block that holds an infinity or a NaN has scale 255 and is NaN
  * throughout.
  *
  * A session over 4-bit rows: sonic_kv_compact_q4 after the prefill, then
