@@ -208,7 +208,7 @@ hipError_t launch_compact(int batch, int total_tokens, int max_seqlen, int Hkv, 
                           uint8_t *vscale, const int64_t *row_off,
                           const int32_t *row_cap, int32_t *cache_len, int32_t *keep_idx, int32_t *status,
                           hipStream_t stream) {
-  const int chunks = max(1, (max_seqlen + kCompactChunk - 1) / kCompactChunk);
+  const int chunks = static_cast<int>(max(1L, (static_cast<long>(max_seqlen) + kCompactChunk - 1) / kCompactChunk));
   const long cb = static_cast<long>(chunks) * batch;
   // (a slice reads the roles before its chunk again; of 4-bit rows it stores a quarter, and half as many are faster: 4
   // requests of 40,320 tokens 42.4 us with their reading back, with 2,048 workgroups 44.8)

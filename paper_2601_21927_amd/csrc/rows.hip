@@ -86,14 +86,14 @@ __global__ __launch_bounds__(kRowThreads) void compact_weights_kernel(
       raise_status(status, len > max_rows ? SONIC_ERR_INVALID_ARG : SONIC_ERR_BAD_LAYOUT);
     return;
   }
-  const int j = blockIdx.x * kRowThreads + threadIdx.x;
-  if (j >= len) return;
-  const int p = keep_idx[off + j];
-  const bool in = p >= 0 && p < e - s;
-  if (ERRORS) {
-    if (!in) raise_status(status, SONIC_ERR_BAD_LAYOUT);
-  } else if (in) {
-    row_weight[off + j] = key_weight[s + p];
+  for (long j = static_cast<long>(blockIdx.x) * kRowThreads + threadIdx.x; j < len; j += static_cast<long>(gridDim.x) * kRowThreads) {
+    const int p = keep_idx[off + j];
+    const bool in = p >= 0 && p < e - s;
+    if (ERRORS) {
+      if (!in) raise_status(status, SONIC_ERR_BAD_LAYOUT);
+    } else if (in) {
+      row_weight[off + j] = key_weight[s + p];
+    }
   }
 }
 
@@ -172,7 +172,9 @@ hipError_t launch_expand_q4(int batch, int max_rows, int Hkv, int D, const uint8
 hipError_t launch_compact_weights(int batch, int total_tokens, int max_rows, const int32_t *cu, const float *key_weight,
                                   const int64_t *row_off, const int32_t *cache_len, const int32_t *keep_idx, float *row_weight,
                                   int32_t *status, hipStream_t stream) {
-  const dim3 grid(std::max(1, (max_rows + kRowThreads - 1) / kRowThreads), batch);
+  // (max_rows is the caller's bound, and may be any number)
+  const long chunks = (static_cast<long>(max_rows) + kRowThreads - 1) / kRowThreads;
+  const dim3 grid(std::max(1L, std::min(chunks, std::max(16L, 4096L / batch))), batch);
   compact_weights_kernel<false><<<grid, dim3(kRowThreads), 0, stream>>>(cu, key_weight, row_off, cache_len, keep_idx, row_weight,
                                                                         total_tokens, max_rows, status);
   const hipError_t e = hipGetLastError();
@@ -185,8 +187,8 @@ hipError_t launch_compact_weights(int batch, int total_tokens, int max_rows, con
 hipError_t launch_add_weights(int batch, int Hq, int max_ctx, const int64_t *row_off, const DecodeRows &rows, float *row_weight,
                               hipStream_t stream) {
   const float inv = 1.f / static_cast<float>(Hq);
-  auto blocks = [&](int k) { return (max_ctx + 16 * k * kWeightWaves - 1) / (16 * k * kWeightWaves); };
-  if (static_cast<long>(blocks(1)) * batch <= 1024)
+  auto blocks = [&](long k) { return (max_ctx + 16 * k * kWeightWaves - 1) / (16 * k * kWeightWaves); };
+  if (blocks(1) * batch <= 1024)
     add_weights_kernel<1><<<dim3(blocks(1), batch), dim3(kWave * kWeightWaves), 0, stream>>>(row_off, rows, row_weight, Hq, inv);
   else
     add_weights_kernel<4><<<dim3(blocks(4), batch), dim3(kWave * kWeightWaves), 0, stream>>>(row_off, rows, row_weight, Hq, inv);
