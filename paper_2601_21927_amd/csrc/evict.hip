@@ -83,20 +83,16 @@ __device__ __forceinline__ void find_digit(int *copies, int need, Digit *found, 
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, EvictWs ws) {
   __shared__ int lds[2 * (kSelectThreads / kWave)];
   __shared__ __align__(8) int copies[kCopies * kBins];
-  __shared__ int s_ok, s_first;
+  __shared__ int s_first;
   __shared__ Digit s_digit;
   const int b = blockIdx.x;
-  // Behind a pending error a length may be anything: no weight is read for it.  Workgroup 0's look decides for the call;
-  // a request whose workgroup saw an error that workgroup 0 did not (the word may change meanwhile) is left as it is.
-  if (!block_status_clear(c.status, &s_ok)) {
-    if (threadIdx.x == 0) {
-      if (b == 0) ws.ctrl[0] = 0;
-      ws.req[b] = make_int2(-1, 0);
-    }
-    return;
-  }
+  // Behind a pending error a length may be anything: no weight is read for it.  Workgroup 0's look at the status word
+  // decides for the call; a request whose workgroup saw an error that workgroup 0 did not (the word may change meanwhile)
+  // is left as it is.
+  const bool pending = __hip_atomic_load(c.status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0;
   EvictReq own;
   const int own_code = evict_check(b, c, &own);
+  if (pending) own.len = own.head = own.tail = 0;
   const float *w = c.row_weight + c.row_off[b];
   const int lo = own.head, hi = own.len - own.tail;
   // A thread has kSelectRows consecutive rows of a chunk; the first chunk's keys stay in registers.  Head and tail
@@ -117,7 +113,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, Evi
   };
   uint32_t first_keys[kSelectRows];
   load_keys(0, first_keys);
-  int bad = 0;
+  int bad = pending;
   for (int j = threadIdx.x; j < c.batch; j += kSelectThreads) {
     EvictReq r;
     bad |= evict_check(j, c, &r) != 0;
@@ -127,7 +123,10 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictCall c, Evi
   bad = __syncthreads_or(bad);
   if (own_code != 0 && threadIdx.x == 0) raise_status(c.status, own_code);
   if (b == 0 && threadIdx.x == 0) ws.ctrl[0] = !bad;
-  if (bad) return;
+  if (bad) {
+    if (threadIdx.x == 0) ws.req[b] = make_int2(-1, 0);
+    return;
+  }
 
   int32_t *list = ws.list + static_cast<size_t>(b) * c.max_rows;
   const int take = own.kept - own.head - own.tail;   // of the middle rows

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kRowThreads) void expand_q4_kernel(
 }
 
 // row_weight of request b's row j = the key weight of the prompt position keep_idx holds for it.  ERRORS: raises what is
-// wrong, behind the launch that writes (see expand_errors_kernel).
+// wrong, behind the launch that writes (see expand_errors_kernel); a word that holds an error keeps it.
 template <bool ERRORS>
 __global__ __launch_bounds__(kRowThreads) void compact_weights_kernel(
     const int32_t *__restrict__ cu, const float *__restrict__ key_weight, const int64_t *__restrict__ row_off,
@@ -80,13 +80,13 @@ __global__ __launch_bounds__(kRowThreads) void compact_weights_kernel(
   const int b = blockIdx.y;
   const int s = cu[b], e = cu[b + 1], len = cache_len[b];
   const int64_t off = row_off[b];
-  if (!block_status_clear(status, &s_ok)) return;
+  if (!ERRORS && !block_status_clear(status, &s_ok)) return;
   if (s < 0 || e < s || e > total_tokens || len < 0 || len > max_rows) {
     if (ERRORS && blockIdx.x == 0 && threadIdx.x == 0)
       raise_status(status, len > max_rows ? SONIC_ERR_INVALID_ARG : SONIC_ERR_BAD_LAYOUT);
     return;
   }
-  for (long j = static_cast<long>(blockIdx.x) * kRowThreads + threadIdx.x; j < len; j += static_cast<long>(gridDim.x) * kRowThreads) {
+  for (unsigned j = blockIdx.x * kRowThreads + threadIdx.x; j < static_cast<unsigned>(len); j += gridDim.x * kRowThreads) {
     const int p = keep_idx[off + j];
     const bool in = p >= 0 && p < e - s;
     if (ERRORS) {
