@@ -50,7 +50,7 @@
  *   first use.  While it is non-zero every later kernel of this library that
  *   receives it returns without writing its outputs, so an error is sticky until
  *   the caller clears it.  The one exception is a pending SONIC_ERR_CAPACITY in
- *   sonic_compressed_decode, where capacity is a per-request matter (see there).
+ *   the decode calls, where capacity is a per-request matter (see sonic_compressed_decode).
  * - softmax_scale: 0 selects the standard scale 1/sqrt(head_dim); any other value
  *   must be finite and positive.
  * - Setting the environment variable SONIC_DEBUG_SYNC=1 makes each GPU call
@@ -103,9 +103,11 @@ enum {
 };
 
 /*
- * Version of this ABI, bumped on any change of a signature, of a layout or of what a call does.
- * Entry points added beside the others leave it as it is: a program that was built before them runs
- * unchanged, and one that needs them finds out by their names.
+ * Version of this ABI, bumped on any change of a signature, of a layout or of what a call does.  Up
+ * to 10 it rose with every entry point that was added as well.  Those of the last two sections (4-bit
+ * rows, row weights and eviction: sonic_kv_compact_q4 to sonic_cache_evict) came to version 10 without
+ * a new number: a program that was built before them runs unchanged, and one that needs them looks
+ * for their names.
  */
 int32_t sonic_abi_version(void);
 
@@ -294,7 +296,10 @@ int32_t sonic_nexus_recon_targets(int32_t batch, int32_t total_tokens, int32_t h
  *   keep_idx                         device int32 [rows], written at kept rows
  *   dev_status                       device int32; SONIC_ERR_CAPACITY when a
  *                                    request keeps more rows than its capacity
- *                                    (no row beyond the capacity is written)
+ *                                    (no row beyond the capacity is written).
+ *                                    After an error that the call itself raised,
+ *                                    the other requests' rows and lengths are not
+ *                                    to be relied on: a part of them is written
  */
 int32_t sonic_kv_compact(int32_t batch, int32_t total_tokens, int32_t max_seqlen, int32_t num_kv_heads,
                          int32_t head_dim, const int32_t *cu_seqlens, const uint8_t *role, const void *k,

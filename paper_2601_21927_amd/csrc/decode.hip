@@ -79,7 +79,10 @@ DecodeShape decode_shape(int batch, int Hkv, int G, int D, int max_ctx, bool mas
 //   rows in one range 30.3 and 26.4).
 // - 256 pairs and more with long contexts share the rows evenly (see decode_shape) among 1,024 workgroups of four waves,
 //   all of them resident: 64 of 180 .. 4,300 rows 36.7 us, with 768 workgroups 39.9, 1,536 38.1 and a range
-//   per pair and 512 rows 39.
+//   per pair and 512 rows 39.  More requests or pairs than that, or shorter contexts, keep a range per pair, which evens out
+//   by itself: 128 of 180 .. 4,300 rows 69 us a step and in three ranges each (what bf16 rows take) 89, 128 of 4,000 142 and
+//   156, 512 of 100 .. 2,500 155 and 263, 64 of 180 .. 4,300 with 16 kv-heads 68 and 81, 128 of 100 under a bound of 4,096
+//   20 and 52, 70 of 100 .. 8,000 69 and 69.
 DecodeShape decode_shape_q4(int batch, int Hkv, int G, int D, int max_ctx) {
   DecodeShape sh{1, 0, 4, 0};
   const long pairs = static_cast<long>(batch) * Hkv;

@@ -5,14 +5,18 @@
 // select_kernel, one workgroup per request: checks the lengths of every request, so that a call is done for all or
 // for none, finds the weight that separates kept from dropped rows by a radix search over the weights' order (up to
 // three passes of eleven bits, histograms in LDS; a request's first 8,192 weights stay in registers), and lists the kept
-// rows.  It writes to the workspace only.  Bound by its chain of barriers and round trips: 11 us for 8 requests of 1,328
-// rows, 12 for 4 of 7,552, 39 for one of 30,000, 102 for one of 100,000.
+// rows.  It writes to the workspace only.  Bound by round trips that wait for one another (status and length, limits,
+// capacity, first row, weights, then three for the other requests' limits; the early returns of evict_check keep the loads
+// apart) and by the search's barriers: 9.5 us for 8 requests of 1,328 rows, 12 for 4 of 7,552, 39 for one of 30,000, 102
+// for one of 100,000.
 // move_kernel, to another cache: every kept row is read and written once, in parallel over rows.  Bound by HBM: 64
-// uneven requests of up to 8,192 rows of 8 bf16 heads of 128 (652 MB) 4.8 TB/s.
+// uneven requests of up to 8,192 rows of 8 bf16 heads of 128 (652 MB) 4.7 TB/s.  Small calls are bound by round trips: a
+// piece's list entry is waited for before its loads, so the pieces of a thread come one after the other.
 // move_in_place_kernel: row j goes down to j from list[j] >= j, so a workgroup that walks the rows upwards, loading a
 // batch before it stores it, never overwrites a row it has yet to read; workgroups split the rows' bytes into
 // columns.  Rows before the first dropped one are not touched.  64 requests of 4,000 bf16 rows to 2,000: 4.5 TB/s; one
-// request has 32 to 64 columns, each a workgroup that waits for its own loads: 30,000 bf16 rows to 20,000 62 us (2.6 TB/s).
+// request has 32 to 64 columns, each a workgroup that waits for its loads and, between a batch's guarded stores, for every
+// store: 30,000 bf16 rows to 20,000 62 us (2.6 TB/s).
 #include <algorithm>
 
 #include "common.h"
@@ -293,7 +297,9 @@ __device__ __forceinline__ void walk_down(UNIT *plane, size_t row0, int row_unit
       if (from[n] >= 0) x[n] = p[static_cast<size_t>(from[n]) * row_units];
     }
     look_up(j0 + rows * kWalkUnroll);
-    __syncthreads();   // the batch is loaded by every thread: rows below j0 + rows * kWalkUnroll may be overwritten
+    // Every thread's loads of the batch come before any store behind the barrier (they need not have arrived: a
+    // workgroup's accesses keep their order): rows below j0 + rows * kWalkUnroll may be overwritten.
+    __syncthreads();
 #pragma unroll
     for (int n = 0; n < kWalkUnroll; ++n)
       if (to[n] >= 0) p[static_cast<size_t>(to[n]) * row_units] = x[n];

@@ -1,6 +1,7 @@
-// Cache rows read back and weighed: 4-bit rows to bf16 (bound by HBM: 30,208 rows of 4 heads of 128, 78 MB, 14.3 us, 5.5
-// TB/s), the prefill's key weights to the rows they were compacted to (three dependent round trips, 3 us), and the
-// attention weights of a decode step added to its rows (4 to 8 us).
+// Cache rows read back and weighed: 4-bit rows to bf16 (bound by HBM: 30,208 rows of 4 heads of 128, 78 MB, 14.4 us, 5.4
+// TB/s, and 1.2 for the launch that raises errors), the prefill's key weights to the rows they were compacted to (three
+// dependent round trips, 3.6 us, and 2.1 for the errors), and the attention weights of a decode step added to its rows (4 to
+// 8 us).
 #include <algorithm>
 
 #include "common.h"
@@ -101,7 +102,8 @@ __global__ __launch_bounds__(kRowThreads) void compact_weights_kernel(
 // exp2(score - normaliser); the appended row's starts there.  Requests the step did not advance (fresh 0) are left
 // alone.  A wave takes K blocks of 16 rows: lane l has rows 4 (l % 4) .. + 3 of heads l / 4, l / 4 + 16, .., and the
 // lanes' sums are added by exchanges in a fixed order, so they do not depend on timing.  Bound by the launch and its
-// round trips (length, scores and normalisers, old weight): 8 requests of 1,328 rows 4 us with K = 1, 5 with K = 4.
+// round trips, one after the other (scores and normalisers of 16 heads at a time, K = 1: then the length, the old weight):
+// 8 requests of 1,328 rows, 32 heads, 4 us with K = 1, 5 with K = 4.
 constexpr int kWeightWaves = 4;
 template <int K>
 __global__ __launch_bounds__(kWave *kWeightWaves) void add_weights_kernel(const int64_t *__restrict__ row_off, DecodeRows rows,
