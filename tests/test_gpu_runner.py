@@ -7,7 +7,7 @@ from oracle import evict as OE
 from paper_2601_21927_amd import sonic
 from paper_2601_21927_amd.runner import bf16_to_device
 from tests import gpu_helpers as H
-from tests.test_gpu_q4 import Cache, i32, normal_bits
+from tests.test_gpu_q4 import EPS, Cache, i32, normal_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +131,34 @@ def test_weights_are_not_made_under_capture():
     assert c.dev.row_weight is None
     assert c.dev.decode_weighted(q, k, v, out, c.status, c.max_ctx) == sonic.OK
     assert c.dev.length.tolist() == [21, 31] and bool((c.dev.row_weight > 0).any())
+
+
+@pytest.mark.parametrize("q4", [True, False])
+def test_two_caches_on_two_streams_at_once(q4):
+    H.need_gpu()
+    rng = np.random.default_rng(39 + q4)
+    caches = [Cache(rng, lens, 8, 2, 64, q4) for lens in ([700, 30, 3000], [5, 4000, 60])]
+    side = [torch.cuda.Stream() for _ in caches]
+    inputs = [[[normal_bits(rng, 3, h, 64) for h in (8, 2, 2)] for _ in range(6)] for _ in caches]
+    dev = [[[bf16_to_device(x) for x in step] for step in steps] for steps in inputs]
+    outs = [[torch.zeros((3, 8, 64), device="cuda") for _ in range(6)] for _ in caches]
+    torch.cuda.synchronize()
+    for t in range(6):
+        for c, s, d, o in zip(caches, side, dev, outs):
+            args = (*d[t], o[t], c.status, c.max_ctx)
+            assert (c.dev.decode(*args, weighted=True, stream=s) if q4 else c.dev.decode_weighted(*args, stream=s)) == sonic.OK
+    torch.cuda.synchronize()
+    for c, steps, o in zip(caches, inputs, outs):
+        got = c.dev.row_weight.cpu().numpy()
+        full = c.weight.astype(np.float64)
+        for t, (q, k, v) in enumerate(steps):
+            for b in range(3):
+                want, w = c.expect(b, q, k, v)
+                rows = slice(int(c.off[b]), int(c.off[b]) + len(w))
+                full[rows.stop - 1] = 0.0
+                full[rows] += w
+                assert np.all(np.abs(o[t][b].cpu().numpy() - want) <= 2 * EPS * np.abs(c.values[1][rows]).max())
+                c.lens[b] += 1
+        # six weights, each within 2 EPS of itself, and a rounding for each sum
+        assert np.all(np.abs(got - full) <= 2 * EPS * (full - np.where(full == c.weight, full, 0)) + 6 * 2.0 ** -24 * full)
+        assert np.array_equal(c.dev.length.cpu().numpy(), c.lens)
