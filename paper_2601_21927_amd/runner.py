@@ -162,7 +162,10 @@ def _evict(cache, keep_head, keep_tail, budget, status, stream, **scales) -> int
 
 
 class CompactCache:
-    """Per-request cache rows [row_off[b], row_off[b] + row_cap[b]) of a [rows, Hkv, d] bf16 pair."""
+    """Per-request cache rows [row_off[b], row_off[b] + row_cap[b]) of a [rows, Hkv, d] bf16 pair.
+
+    row_weight (fp32 [rows], for decode_weighted and evict; None until decode_weighted or the caller makes it) is the caller's
+    to set after a compaction: sonic.kv_compact_weights, or zeros."""
 
     def __init__(self, rows, Hkv, d, row_off, row_cap, device, fill_bits=0xFFFF):
         self.rows, self.Hkv, self.d = rows, Hkv, d
@@ -208,7 +211,8 @@ class CompactCache:
 
 
 class Q4Cache:
-    """The same rows in 4 bits: codes [rows, Hkv, d / 2] and scale bytes [rows, Hkv, d / 32] of K and V."""
+    """The same rows in 4 bits: codes [rows, Hkv, d / 2] and scale bytes [rows, Hkv, d / 32] of K and V.  row_weight as in
+    CompactCache, zeros at first."""
 
     def __init__(self, rows, Hkv, d, row_off, row_cap, device):
         self.rows, self.Hkv, self.d = rows, Hkv, d
