@@ -24,6 +24,10 @@
  * attention its rows received (sonic_kv_compact_weights,
  * sonic_compressed_decode_weighted, sonic_cache_evict).
  *
+ * A generation step may also verify several drafted tokens of every request at once
+ * (sonic_tree_plan, sonic_tree_decode, sonic_logits_process, sonic_tree_accept,
+ * sonic_cache_append).
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - Pointers marked "device" are HIP device pointers; "host" pointers are CPU
@@ -50,7 +54,8 @@
  *   first use.  While it is non-zero every later kernel of this library that
  *   receives it returns without writing its outputs, so an error is sticky until
  *   the caller clears it.  The one exception is a pending SONIC_ERR_CAPACITY in
- *   the decode calls, where capacity is a per-request matter (see sonic_compressed_decode).
+ *   the decode calls and those of a step over drafted tokens, where capacity is a
+ *   per-request matter (see sonic_compressed_decode).
  * - softmax_scale: 0 selects the standard scale 1/sqrt(head_dim); any other value
  *   must be finite and positive.
  * - Setting the environment variable SONIC_DEBUG_SYNC=1 makes each GPU call
@@ -104,10 +109,10 @@ enum {
 
 /*
  * Version of this ABI, bumped on any change of a signature, of a layout or of what a call does.  Up
- * to 10 it rose with every entry point that was added as well.  Those of the last two sections (4-bit
- * rows, row weights and eviction: sonic_kv_compact_q4 to sonic_cache_evict) came to version 10 without
- * a new number: a program that was built before them runs unchanged, and one that needs them looks
- * for their names.
+ * to 10 it rose with every entry point that was added as well.  Those of the last three sections (4-bit
+ * rows, row weights and eviction, drafted tokens: sonic_kv_compact_q4 to sonic_cache_append) came to
+ * version 10 without a new number: a program that was built before them runs unchanged, and one that
+ * needs them looks for their names.
  */
 int32_t sonic_abi_version(void);
 
@@ -602,6 +607,156 @@ int32_t sonic_cache_evict(int32_t batch, int32_t max_rows, int32_t num_kv_heads,
                           const int64_t *out_row_off, const int32_t *out_row_cap, int32_t *out_len, float *out_weight,
                           int32_t *keep_idx, void *workspace, size_t workspace_bytes, int32_t *dev_status,
                           void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* A step over drafted tokens                                                */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * A program that drafts tokens (with a small model, or from the text so far) has the model look at all of them in
+ * one step and keeps those that it would have generated itself.  The drafted tokens of a request ("nodes") form a
+ * tree, or several: every node continues its parent's text.  One step is
+ *   sonic_tree_plan         once: which nodes every node sees
+ *   sonic_tree_decode       per layer: the nodes' attention over the cache and their own paths
+ *   sonic_logits_process    penalties, biases and masks on the nodes' logits, and each node's best token
+ *   sonic_tree_accept       the path of nodes that the chosen tokens confirm, and the token after it
+ *   sonic_cache_append      per layer: that path's K and V to the end of the cache
+ * and needs no host round trip.  A chain of nodes is also a piece of a prompt taken over an existing cache:
+ * sonic_tree_decode, then sonic_cache_append of all its rows.
+ *
+ * Nodes are packed over the batch: request b's are cu_nodes[b] .. cu_nodes[b+1]-1.  total_nodes is a host bound,
+ * cu_nodes[B] <= total_nodes, so that a captured step serves trees of other sizes; rows of an output past cu_nodes[B]
+ * are left as they were.  In all of these calls a pending SONIC_ERR_CAPACITY stops nothing; any other pending error
+ * stops the call: nothing is written.
+ */
+
+/* Bytes of a plan (0 for negative sizes). */
+size_t sonic_tree_plan_bytes(int32_t batch, int32_t total_nodes, int32_t max_nodes);
+
+/*
+ * The plan of a step, for the calls below; node i of a request sees itself and its ancestors.
+ *   max_nodes     host bound on a request's nodes, at most 256
+ *   cu_nodes      device int32 [B+1], non-decreasing, cu_nodes[0] = 0; a request may have no nodes
+ *   parent        device int32 [total_nodes]: a node's parent as a place in its request (0 its first node), smaller than
+ *                 the node's own, or -1 for a root; NULL: every request's nodes are a chain, each the child of the one before
+ *   plan          device, 256-byte aligned, >= sonic_tree_plan_bytes(B, total_nodes, max_nodes) bytes; the calls that
+ *                 take it are given the same B, total_nodes and max_nodes
+ *   dev_status    SONIC_ERR_BAD_LAYOUT for inconsistent cu_nodes, a request of more than max_nodes nodes, or a parent that
+ *                 does not come before its node; such a request has no nodes in the plan, and the others' parts are not to be
+ *                 relied on either
+ * Returns SONIC_ERR_UNSUPPORTED for max_nodes > 256 and SONIC_ERR_WORKSPACE for a plan that is too small, as the calls that
+ * take it do.
+ */
+int32_t sonic_tree_plan(int32_t batch, int32_t total_nodes, int32_t max_nodes, const int32_t *cu_nodes, const int32_t *parent,
+                        void *plan, size_t plan_bytes, int32_t *dev_status, void *stream);
+
+/* Bytes of device workspace sonic_tree_decode needs (any Hkv dividing Hq). */
+size_t sonic_tree_decode_workspace_bytes(int32_t batch, int32_t max_nodes, int32_t num_q_heads, int32_t head_dim, int32_t max_ctx);
+
+/*
+ * For every node i of every request b and q-head h
+ *     out[i][h] = softmax_r(scale * <q[i][h], k[r][g(h)]>) v[r][g(h)]
+ * over the request's cache rows 0 .. cache_len[b] - 1 and the rows k_new, v_new of the nodes that i sees.  The cache is
+ * only read: sonic_cache_append adds the rows that are kept.
+ *   max_ctx         host bound: cache_len[b] <= max_ctx for every b; 0 for empty caches
+ *   k_cache, v_cache   device bf16 [rows][Hkv][d] with k_scale = v_scale = NULL, or 4-bit rows with their scales; then the
+ *                   nodes' rows are rounded as sonic_cache_append would, and take part at their 4-bit values
+ *   q               device bf16 [total_nodes][Hq][d];  k_new, v_new: device bf16 [total_nodes][Hkv][d]
+ *   softmax_scale   0 for 1/sqrt(d), else finite and > 0
+ *   out             device [total_nodes][Hq][d], fp32 (out_bf16 = 0) or bf16 (1, the operand type of sonic_role_projection).
+ *                   Probabilities go into the product in three bf16 values for fp32, which leaves 2^-26 of them, and in
+ *                   one for bf16: the output is then off by about 1.3 times its own rounding
+ *   workspace       device, 256-byte aligned, >= sonic_tree_decode_workspace_bytes(B, max_nodes, Hq, d, max_ctx) bytes;
+ *                   contents need no initialisation.  Calls that share one must not run concurrently
+ *   dev_status      SONIC_ERR_CAPACITY when cache_len[b] is negative or above max_ctx: the request's outputs are
+ *                   not written, the others' are
+ * A value of a node's V that is no number reaches the nodes that see it only.  Reproducible.
+ */
+int32_t sonic_tree_decode(int32_t batch, int32_t total_nodes, int32_t max_nodes, int32_t num_q_heads, int32_t num_kv_heads,
+                          int32_t head_dim, int32_t max_ctx, const void *plan, size_t plan_bytes, const void *k_cache,
+                          const void *k_scale, const void *v_cache, const void *v_scale, const int64_t *cache_row_off,
+                          const int32_t *cache_len, const void *q, const void *k_new, const void *v_new, float softmax_scale,
+                          void *out, int32_t out_bf16, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/* Bytes of device workspace sonic_logits_process needs (0 for negative sizes). */
+size_t sonic_logits_process_workspace_bytes(int32_t total_rows, int32_t vocab);
+
+/*
+ * Logits as a sampler wants them, and the best token of every row.  A row is a node of a plan, or, with plan = NULL,
+ * row b is request b's (total_rows = B).  For a row of request b and token t, with c the number of times that t is
+ * among the request's generated tokens (tokens behind the prompt) and on the row's path (the tokens of its node and of that
+ * node's ancestors; without a plan the row's own token):
+ *     x = logits[row][t]
+ *     t in the prompt, or c > 0:   x = x > 0 ? x / repetition[b] : x * repetition[b]
+ *     c > 0:                       x = x - (presence[b] + frequency[b] * c)
+ *     t has a bias:                x = x + bias
+ *     t is not allowed:            x = -infinity
+ * each operation in fp32, rounded by itself.  A token outside of 0 .. vocab - 1 counts for nothing.
+ *   max_nodes       that of the plan (ignored without one)
+ *   logits          device [total_rows][vocab], fp32 (logits_bf16 = 0) or bf16 (1), 16-byte aligned; any vocab up to 2^28
+ *   node_token      NULL (rows have no path), or device int32 [total_rows]: the rows' tokens
+ *   tokens          NULL (no history), or device int32: request b's history is tokens[token_off[b]] .., token_len[b] of them,
+ *                   the first prompt_len[b] the prompt (prompt_len NULL: none)
+ *   token_off       device int64 [B];  token_len, prompt_len: device int32 [B]
+ *   repetition, presence, frequency   NULL (1, 0, 0), or device fp32 [B]
+ *   bias_cu         NULL (no biases), or device int32 [B+1]: request b's entries of bias_token (device int32) and bias_value
+ *                   (device fp32) are bias_cu[b] .. bias_cu[b+1]-1; of several entries for one token the last counts
+ *   allowed         NULL (all), or device uint32 [total_rows][(vocab + 31) / 32]: bit t % 32 of word t / 32 allows token t
+ *   out             NULL, or device fp32 [total_rows][vocab], 16-byte aligned (not the logits): x
+ *   best            NULL, or device int32 [total_rows]: the lowest token of the greatest x (a NaN counts as -infinity), -1
+ *                   where no x is above -infinity
+ *   best_value      NULL, or device fp32 [total_rows]: its x, -infinity for -1
+ *   workspace       device, 256-byte aligned, >= sonic_logits_process_workspace_bytes(total_rows, vocab) bytes; contents need
+ *                   no initialisation.  Calls that share one must not run concurrently
+ *   dev_status      SONIC_ERR_BAD_LAYOUT for a negative token_len, a prompt_len outside of 0 .. token_len[b], or
+ *                   inconsistent bias_cu: nothing is written for that request's rows, the others are done
+ */
+int32_t sonic_logits_process(int32_t batch, int32_t total_rows, int32_t max_nodes, int32_t vocab, const void *logits,
+                             int32_t logits_bf16, const void *plan, size_t plan_bytes, const int32_t *node_token,
+                             const int32_t *tokens, const int64_t *token_off, const int32_t *token_len, const int32_t *prompt_len,
+                             const float *repetition, const float *presence, const float *frequency, const int32_t *bias_cu,
+                             const int32_t *bias_token, const float *bias_value, const void *allowed, float *out, int32_t *best,
+                             float *best_value, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * The nodes that the chosen tokens confirm.  The path of request b starts with its node 0, whose token was chosen by the
+ * step before; from the path's last node i on, it goes to the lowest child of i whose token is chosen[i], until there is none.
+ *   parent          as for the plan (NULL: chains)
+ *   node_token      device int32 [total_nodes]: the nodes' tokens
+ *   chosen          device int32 [total_nodes]: for every node the token that follows it (sonic_logits_process's best, or
+ *                   a sampler's)
+ *   path            device int32 [total_nodes]: request b's path, places in the request, at cu_nodes[b] ..; -1 behind it
+ *   path_len        device int32 [B]: nodes of the path, 0 for a request without nodes
+ *   next_token      device int32 [B]: chosen[the path's last node], the first token of the next step; -1 without nodes
+ *   tokens ..       NULL, all four, or the requests' histories (as for sonic_logits_process), of which request b owns
+ *                   token_cap[b] places: the path's tokens are added and token_len[b] is advanced
+ *   dev_status      SONIC_ERR_CAPACITY when a history has no room for the path: the request's path_len is 0, its
+ *                   next_token -1, its history as it was; the others are done
+ */
+int32_t sonic_tree_accept(int32_t batch, int32_t total_nodes, int32_t max_nodes, const void *plan, size_t plan_bytes,
+                          const int32_t *parent, const int32_t *node_token, const int32_t *chosen, int32_t *path, int32_t *path_len,
+                          int32_t *next_token, int32_t *tokens, const int64_t *token_off, const int32_t *token_cap,
+                          int32_t *token_len, int32_t *dev_status, void *stream);
+
+/*
+ * New rows to the end of every request's cache: cache row cache_row_off[b] + cache_len[b] + j takes new row
+ * new_cu[b] + select[new_cu[b] + j], for j < select_len[b], and cache_len[b] is advanced by that many.
+ *   max_rows        host bound on the rows appended to a request
+ *   new_cu          device int32 [B+1], non-decreasing, new_cu[B] <= total_new: request b's new rows
+ *   select          NULL together with select_len: all of them, in order; or device int32 [total_new] and [B]
+ *                   (sonic_tree_accept's path and path_len): places in the request's new rows, in any order, also
+ *                   several times; select_len[b] is at most the request's new rows
+ *   k_new, v_new    device bf16 [total_new][Hkv][d]
+ *   k_cache ..      bf16 rows with k_scale = v_scale = NULL, or 4-bit rows with their scales: then the rows are rounded
+ *   dev_status      SONIC_ERR_BAD_LAYOUT for inconsistent new_cu, a negative length, or a select or select_len out of
+ *                   range, SONIC_ERR_INVALID_ARG for more than max_rows rows, SONIC_ERR_CAPACITY for more than
+ *                   cache_row_cap[b] - cache_len[b]: the request is left unchanged, the others are done
+ */
+int32_t sonic_cache_append(int32_t batch, int32_t total_new, int32_t max_rows, int32_t num_kv_heads, int32_t head_dim,
+                           const int32_t *new_cu, const int32_t *select, const int32_t *select_len, const void *k_new,
+                           const void *v_new, void *k_cache, void *k_scale, void *v_cache, void *v_scale,
+                           const int64_t *cache_row_off, const int32_t *cache_row_cap, int32_t *cache_len, int32_t *dev_status,
+                           void *stream);
 
 #ifdef __cplusplus
 }

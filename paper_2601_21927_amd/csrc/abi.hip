@@ -64,6 +64,16 @@ hipError_t launch_compact_weights(int batch, int total_tokens, int max_rows, con
                                   const int64_t *row_off, const int32_t *cache_len, const int32_t *keep_idx, float *row_weight,
                                   int32_t *status, hipStream_t stream);
 hipError_t launch_evict(const EvictCall &c, const EvictWs &ws, int Hkv, int D, hipStream_t stream);
+hipError_t launch_tree_plan(int batch, int total, int max_nodes, const int32_t *cu, const int32_t *parent, TreePlan plan,
+                            int32_t *status, hipStream_t stream);
+TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ctx);
+hipError_t launch_tree(const TreeCall &c, const TreeShape &sh, float *part, int Hkv, int G, int D, hipStream_t stream);
+hipError_t launch_tree_accept(int batch, int total, int max_nodes, TreePlan plan, const int32_t *parent, const int32_t *node_token,
+                              const int32_t *chosen, int32_t *path, int32_t *path_len, int32_t *next_token, int32_t *tokens,
+                              const int64_t *token_off, const int32_t *token_cap, int32_t *token_len, int32_t *status, hipStream_t stream);
+hipError_t launch_append(const AppendCall &c, int Hkv, int D, hipStream_t stream);
+int logits_pieces(int vocab);
+hipError_t launch_logits(const LogitsCall &c, void *workspace, hipStream_t stream);
 
 namespace {
 
@@ -885,6 +895,166 @@ int32_t sonic_cache_evict(int32_t batch, int32_t max_rows, int32_t Hkv, int32_t 
                     static_cast<uint8_t *>(k_scale_out), static_cast<uint8_t *>(v_scale_out), out_row_off, out_row_cap, out_len,
                     out_weight, keep_idx, dev_status};
   return finish(launch_evict(c, ws, Hkv, d, stream), dev_status, stream);
+}
+
+// ---------------------------------------------------------------- a step over drafted tokens
+// The plan: each request's first node and nodes, then the nodes' words.
+static size_t tree_plan_layout(int32_t batch, int32_t total, int32_t max_nodes, const void *base, TreePlan *plan) {
+  const size_t r_bytes = align_up(static_cast<size_t>(batch) * sizeof(int2), 256);
+  const int words = (max_nodes + 31) / 32;
+  if (plan) {
+    plan->req = static_cast<const int2 *>(base);
+    plan->sees = reinterpret_cast<const uint32_t *>(static_cast<const char *>(base) + r_bytes);
+    plan->words = words;
+  }
+  return align_up(r_bytes + static_cast<size_t>(total) * words * sizeof(uint32_t) + 256, 256);
+}
+
+size_t sonic_tree_plan_bytes(int32_t batch, int32_t total_nodes, int32_t max_nodes) {
+  if (batch < 0 || total_nodes < 0 || max_nodes < 0) return 0;
+  return tree_plan_layout(batch, total_nodes, max_nodes, nullptr, nullptr);
+}
+
+// What every call on a plan checks of it.
+static int32_t check_plan(int32_t batch, int32_t total, int32_t max_nodes, const void *plan, size_t plan_bytes, const int32_t *dev_status) {
+  if (batch < 0 || total < 0 || max_nodes < 0 || dev_status == nullptr) return SONIC_ERR_INVALID_ARG;
+  if (batch > 65535 || max_nodes > kMaxNodes) return SONIC_ERR_UNSUPPORTED;
+  if (batch == 0) return SONIC_OK;
+  if (!plan || !aligned(plan, 256)) return SONIC_ERR_INVALID_ARG;
+  return plan_bytes < tree_plan_layout(batch, total, max_nodes, nullptr, nullptr) ? SONIC_ERR_WORKSPACE : SONIC_OK;
+}
+
+int32_t sonic_tree_plan(int32_t batch, int32_t total_nodes, int32_t max_nodes, const int32_t *cu_nodes, const int32_t *parent,
+                        void *plan, size_t plan_bytes, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  const int32_t st = check_plan(batch, total_nodes, max_nodes, plan, plan_bytes, dev_status);
+  if (st != SONIC_OK || batch == 0) return st;
+  if (!cu_nodes) return SONIC_ERR_INVALID_ARG;
+  TreePlan p;
+  tree_plan_layout(batch, total_nodes, max_nodes, plan, &p);
+  return finish(launch_tree_plan(batch, total_nodes, max_nodes, cu_nodes, parent, p, dev_status, stream), dev_status, stream);
+}
+
+size_t sonic_tree_decode_workspace_bytes(int32_t batch, int32_t max_nodes, int32_t Hq, int32_t d, int32_t max_ctx) {
+  if (batch <= 0 || max_nodes <= 0 || Hq <= 0 || max_ctx < 0) return 256;
+  size_t part = 0;   // for any kv-head count the call may use
+  for (int hkv = 1; hkv <= Hq; ++hkv)
+    if (Hq % hkv == 0 && Hq / hkv <= 8) part = std::max(part, tree_shape(batch, hkv, Hq / hkv, d, max_nodes, max_ctx).part_bytes);
+  return align_up(part + 256, 256);
+}
+
+int32_t sonic_tree_decode(int32_t batch, int32_t total_nodes, int32_t max_nodes, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_ctx,
+                          const void *plan, size_t plan_bytes, const void *k_cache, const void *k_scale, const void *v_cache,
+                          const void *v_scale, const int64_t *cache_row_off, const int32_t *cache_len, const void *q, const void *k_new,
+                          const void *v_new, float softmax_scale, void *out, int32_t out_bf16, void *workspace, size_t workspace_bytes,
+                          int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (Hq <= 0 || Hkv <= 0 || max_ctx < 0) return SONIC_ERR_INVALID_ARG;
+  if (d != 64 && d != 128) return SONIC_ERR_UNSUPPORTED;
+  if (Hq % Hkv != 0 || (out_bf16 != 0 && out_bf16 != 1)) return SONIC_ERR_INVALID_ARG;
+  if (Hq / Hkv > 8 || Hkv > 65535) return SONIC_ERR_UNSUPPORTED;
+  if (!std::isfinite(softmax_scale) || softmax_scale < 0.f) return SONIC_ERR_INVALID_ARG;
+  softmax_scale = default_scale(softmax_scale, d);
+  const int32_t st = check_plan(batch, total_nodes, max_nodes, plan, plan_bytes, dev_status);
+  if (st != SONIC_OK || batch == 0) return st;
+  if (total_nodes == 0 || max_nodes == 0) return SONIC_OK;
+  if (!k_cache || !v_cache || !cache_row_off || !cache_len || !q || !k_new || !v_new || !out || !workspace) return SONIC_ERR_INVALID_ARG;
+  if ((k_scale != nullptr) != (v_scale != nullptr)) return SONIC_ERR_INVALID_ARG;
+  if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4) || !aligned(q, 16) ||
+      !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(out, 16) || !aligned(workspace, 256))
+    return SONIC_ERR_INVALID_ARG;
+  const TreeShape sh = tree_shape(batch, Hkv, Hq / Hkv, d, max_nodes, max_ctx);
+  if (workspace_bytes < sh.part_bytes) return SONIC_ERR_WORKSPACE;
+  if ((static_cast<long>(batch) * Hkv * sh.splits + kNumXcd) * sh.tiles > INT32_MAX) return SONIC_ERR_UNSUPPORTED;   // the grid
+  TreeCall c{};
+  c.batch = batch, c.total_nodes = total_nodes, c.max_nodes = max_nodes, c.max_ctx = max_ctx;
+  tree_plan_layout(batch, total_nodes, max_nodes, plan, &c.plan);
+  c.k = k_cache, c.v = v_cache;
+  c.ks = static_cast<const uint8_t *>(k_scale), c.vs = static_cast<const uint8_t *>(v_scale);
+  c.row_off = cache_row_off, c.cache_len = cache_len;
+  c.q = static_cast<const uint16_t *>(q), c.k_new = static_cast<const uint16_t *>(k_new), c.v_new = static_cast<const uint16_t *>(v_new);
+  c.scale_log2 = static_cast<float>(softmax_scale * kLog2e);
+  c.out = out, c.out_bf16 = out_bf16 != 0;
+  c.status = dev_status;
+  return finish(launch_tree(c, sh, static_cast<float *>(workspace), Hkv, Hq / Hkv, d, stream), dev_status, stream);
+}
+
+int32_t sonic_tree_accept(int32_t batch, int32_t total_nodes, int32_t max_nodes, const void *plan, size_t plan_bytes,
+                          const int32_t *parent, const int32_t *node_token, const int32_t *chosen, int32_t *path, int32_t *path_len,
+                          int32_t *next_token, int32_t *tokens, const int64_t *token_off, const int32_t *token_cap, int32_t *token_len,
+                          int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  const int32_t st = check_plan(batch, total_nodes, max_nodes, plan, plan_bytes, dev_status);
+  if (st != SONIC_OK || batch == 0) return st;
+  if (!path_len || !next_token || (total_nodes > 0 && (!node_token || !chosen || !path))) return SONIC_ERR_INVALID_ARG;
+  if ((token_off != nullptr) != (tokens != nullptr) || (token_cap != nullptr) != (tokens != nullptr) ||
+      (token_len != nullptr) != (tokens != nullptr))
+    return SONIC_ERR_INVALID_ARG;
+  TreePlan p;
+  tree_plan_layout(batch, total_nodes, max_nodes, plan, &p);
+  return finish(launch_tree_accept(batch, total_nodes, max_nodes, p, parent, node_token, chosen, path, path_len, next_token, tokens,
+                                   token_off, token_cap, token_len, dev_status, stream),
+                dev_status, stream);
+}
+
+int32_t sonic_cache_append(int32_t batch, int32_t total_new, int32_t max_rows, int32_t Hkv, int32_t d, const int32_t *new_cu,
+                           const int32_t *select, const int32_t *select_len, const void *k_new, const void *v_new, void *k_cache,
+                           void *k_scale, void *v_cache, void *v_scale, const int64_t *cache_row_off, const int32_t *cache_row_cap,
+                           int32_t *cache_len, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (batch < 0 || total_new < 0 || max_rows < 0 || Hkv <= 0 || dev_status == nullptr) return SONIC_ERR_INVALID_ARG;
+  if (batch > 65535 || Hkv > 65535) return SONIC_ERR_UNSUPPORTED;
+  if (d != 64 && d != 128) return SONIC_ERR_UNSUPPORTED;
+  if (batch == 0) return SONIC_OK;
+  if (!new_cu || !cache_row_off || !cache_row_cap || !cache_len) return SONIC_ERR_INVALID_ARG;
+  if ((select != nullptr) != (select_len != nullptr) || (k_scale != nullptr) != (v_scale != nullptr)) return SONIC_ERR_INVALID_ARG;
+  if (total_new > 0 && (!k_new || !v_new || !k_cache || !v_cache)) return SONIC_ERR_INVALID_ARG;
+  for (const void *p : {k_new, v_new, static_cast<const void *>(k_cache), static_cast<const void *>(v_cache)})
+    if (!aligned(p, 16)) return SONIC_ERR_INVALID_ARG;
+  if (!aligned(k_scale, 4) || !aligned(v_scale, 4)) return SONIC_ERR_INVALID_ARG;
+  const AppendCall c{batch, total_new, max_rows, new_cu, select, select_len, static_cast<const uint16_t *>(k_new),
+                     static_cast<const uint16_t *>(v_new), k_cache, v_cache, static_cast<uint8_t *>(k_scale),
+                     static_cast<uint8_t *>(v_scale), cache_row_off, cache_row_cap, cache_len, dev_status};
+  return finish(launch_append(c, Hkv, d, stream), dev_status, stream);
+}
+
+size_t sonic_logits_process_workspace_bytes(int32_t total_rows, int32_t vocab) {
+  if (total_rows < 0 || vocab < 0) return 0;
+  return align_up(static_cast<size_t>(total_rows) * logits_pieces(vocab) * 8 + 256, 256);
+}
+
+int32_t sonic_logits_process(int32_t batch, int32_t total_rows, int32_t max_nodes, int32_t vocab, const void *logits, int32_t logits_bf16,
+                             const void *plan, size_t plan_bytes, const int32_t *node_token, const int32_t *tokens,
+                             const int64_t *token_off, const int32_t *token_len, const int32_t *prompt_len, const float *repetition,
+                             const float *presence, const float *frequency, const int32_t *bias_cu, const int32_t *bias_token,
+                             const float *bias_value, const void *allowed, float *out, int32_t *best, float *best_value,
+                             void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream_) {
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (batch < 0 || total_rows < 0 || max_nodes < 0 || vocab <= 0 || dev_status == nullptr) return SONIC_ERR_INVALID_ARG;
+  if (logits_bf16 != 0 && logits_bf16 != 1) return SONIC_ERR_INVALID_ARG;
+  if (batch > 65535 || vocab > kMaxVocab) return SONIC_ERR_UNSUPPORTED;
+  LogitsCall c{};
+  if (plan != nullptr) {
+    const int32_t st = check_plan(batch, total_rows, max_nodes, plan, plan_bytes, dev_status);
+    if (st != SONIC_OK) return st;
+    tree_plan_layout(batch, total_rows, max_nodes, plan, &c.plan);
+  } else if (total_rows != batch) {
+    return SONIC_ERR_INVALID_ARG;   // a row a request
+  } else {
+    max_nodes = 1;
+  }
+  if (batch == 0 || total_rows == 0 || max_nodes == 0) return SONIC_OK;
+  if (!logits || !workspace || (!out && !best && !best_value)) return SONIC_ERR_INVALID_ARG;
+  if (tokens != nullptr ? !token_off || !token_len : token_off || token_len || prompt_len) return SONIC_ERR_INVALID_ARG;
+  if ((bias_token != nullptr) != (bias_cu != nullptr) || (bias_value != nullptr) != (bias_cu != nullptr)) return SONIC_ERR_INVALID_ARG;
+  if (!aligned(logits, 16) || !aligned(out, 16) || !aligned(allowed, 4) || !aligned(workspace, 256)) return SONIC_ERR_INVALID_ARG;
+  if (workspace_bytes < static_cast<size_t>(total_rows) * logits_pieces(vocab) * 8) return SONIC_ERR_WORKSPACE;
+  c.batch = batch, c.total_rows = total_rows, c.max_rows = max_nodes, c.vocab = vocab, c.bf16 = logits_bf16 != 0, c.logits = logits;
+  c.node_token = node_token, c.tokens = tokens, c.token_off = token_off, c.token_len = token_len, c.prompt_len = prompt_len;
+  c.repetition = repetition, c.presence = presence, c.frequency = frequency;
+  c.bias_cu = bias_cu, c.bias_token = bias_token, c.bias_value = bias_value, c.allowed = static_cast<const uint32_t *>(allowed);
+  c.out = out, c.best = best, c.best_value = best_value, c.status = dev_status;
+  return finish(launch_logits(c, workspace, stream), dev_status, stream);
 }
 
 }  // extern "C"

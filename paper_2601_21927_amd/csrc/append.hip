@@ -1,0 +1,118 @@
+// Rows to the end of a cache: the selected new rows of every request behind its rows, bf16 as they are or rounded to 4 bits,
+// and the lengths advanced.  Two launches: every workgroup of the first one reads the lengths that the second advances, and
+// errors are raised by the second, so that one request's error does not keep another's workgroups from writing.
+#include <algorithm>
+
+#include "common.h"
+#include "q4.h"
+
+namespace sonic {
+
+constexpr int kAppendThreads = 256;
+
+// What is appended to request b: `rows` of them, from new row `first` on.  Returns 0 or what is wrong; `select` is looked at
+// by the whole workgroup.
+struct AppendReq {
+  int first, rows, len;
+};
+__device__ __forceinline__ int append_check(const AppendCall &c, int b, AppendReq *r) {
+  const int s = c.new_cu[b], e = c.new_cu[b + 1], len = c.cache_len[b], cap = c.row_cap[b];
+  const int n = c.select != nullptr ? c.select_len[b] : e - s;
+  *r = AppendReq{s, n, len};
+  if (s < 0 || e < s || e > c.total_new || n < 0 || n > e - s || len < 0) return SONIC_ERR_BAD_LAYOUT;
+  if (n > c.max_rows) return SONIC_ERR_INVALID_ARG;
+  if (n > cap - len) return SONIC_ERR_CAPACITY;
+  return 0;
+}
+
+// Grid (chunks of units, requests).  A unit is 16 bytes of a bf16 row, or a quantisation block (64 bytes) of a 4-bit one.
+template <bool Q4>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendCall c, int row_units) {
+  __shared__ int s_go;
+  const int b = blockIdx.y;
+  AppendReq r;
+  const int code = append_check(c, b, &r);
+  const int64_t base = c.row_off[b];
+  if (threadIdx.x == 0) s_go = !step_stops(c.status);
+  __syncthreads();
+  if (!s_go || code != 0) return;
+  const int n_new = c.new_cu[b + 1] - r.first;
+  bool bad = false;
+  if (c.select != nullptr)
+    for (int j = threadIdx.x; j < r.rows; j += kAppendThreads) {
+      const int x = c.select[r.first + j];
+      bad = bad || x < 0 || x >= n_new;
+    }
+  if (__syncthreads_or(bad)) return;
+  const long total = static_cast<long>(r.rows) * row_units;
+  for (long u = static_cast<long>(blockIdx.x) * kAppendThreads + threadIdx.x; u < total; u += static_cast<long>(gridDim.x) * kAppendThreads) {
+    const int j = static_cast<int>(u / row_units), piece = static_cast<int>(u - static_cast<long>(j) * row_units);
+    const size_t from = static_cast<size_t>(r.first + (c.select != nullptr ? c.select[r.first + j] : j)) * row_units + piece;
+    const size_t to = static_cast<size_t>(base + r.len + j) * row_units + piece;
+    if constexpr (!Q4) {
+      const u32x4 k = reinterpret_cast<const u32x4 *>(c.k_new)[from], v = reinterpret_cast<const u32x4 *>(c.v_new)[from];
+      static_cast<u32x4 *>(c.k)[to] = k;
+      static_cast<u32x4 *>(c.v)[to] = v;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32x4 *src = reinterpret_cast<const u32x4 *>(t == 0 ? c.k_new : c.v_new) + from * 4;
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const u32x4 x = src[i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
+        }
+        const uint32_t byte = q4_scale_byte(q4_top(w));
+        u32x4 codes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes[i] = q4_encode8(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3], byte);
+        static_cast<u32x4 *>(t == 0 ? c.k : c.v)[to] = codes;
+        (t == 0 ? c.ks : c.vs)[to] = static_cast<uint8_t>(byte);
+      }
+    }
+  }
+}
+
+// The lengths, or what is wrong with a request: sixteen lanes for each, all in one workgroup, which looks at the status word
+// before it raises anything.
+constexpr int kLengthThreads = 1024, kLengthLanes = 16;
+__global__ __launch_bounds__(kLengthThreads) void append_lengths_kernel(AppendCall c) {
+  __shared__ int s_go;
+  if (threadIdx.x == 0) s_go = !step_stops(c.status);
+  __syncthreads();
+  const int lane = threadIdx.x % kLengthLanes;
+  for (int b0 = 0; b0 < c.batch; b0 += kLengthThreads / kLengthLanes) {
+    const int b = b0 + threadIdx.x / kLengthLanes;
+    AppendReq r{};
+    int code = b < c.batch ? append_check(c, b, &r) : 0;
+    bool bad = false;
+    if (b < c.batch && c.select != nullptr && code == 0) {
+      const int n_new = c.new_cu[b + 1] - r.first;
+#pragma unroll 4
+      for (int j = lane; j < r.rows; j += kLengthLanes) {
+        const int x = c.select[r.first + j];
+        bad = bad || x < 0 || x >= n_new;
+      }
+    }
+    const uint64_t any = __ballot(bad) >> (threadIdx.x % kWave / kLengthLanes * kLengthLanes);
+    if ((any & ((1u << kLengthLanes) - 1)) != 0) code = SONIC_ERR_BAD_LAYOUT;
+    if (lane == 0 && b < c.batch && s_go) {
+      if (code != 0) raise_status(c.status, code);
+      else c.cache_len[b] = r.len + r.rows;
+    }
+  }
+}
+
+hipError_t launch_append(const AppendCall &c, int Hkv, int D, hipStream_t stream) {
+  const int row_units = Hkv * D / (c.ks != nullptr ? kQ4Block : 8);
+  const long chunks = (static_cast<long>(c.max_rows) * row_units + kAppendThreads - 1) / kAppendThreads;
+  const dim3 grid(std::max(1L, std::min(chunks, 64L)), c.batch);
+  if (c.ks != nullptr) append_kernel<true><<<grid, dim3(kAppendThreads), 0, stream>>>(c, row_units);
+  else append_kernel<false><<<grid, dim3(kAppendThreads), 0, stream>>>(c, row_units);
+  append_lengths_kernel<<<dim3(1), dim3(kLengthThreads), 0, stream>>>(c);
+  return hipGetLastError();
+}
+
+}  // namespace sonic

@@ -35,6 +35,12 @@ __device__ __forceinline__ bool block_status_clear(const int32_t *status, int *l
   return *lds_flag != 0;
 }
 
+// The calls of a step over drafted tokens go on behind a pending capacity error, which is one request's matter.
+__device__ __forceinline__ bool step_stops(const int32_t *status) {
+  const int pending = __hip_atomic_load(status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return pending != 0 && pending != SONIC_ERR_CAPACITY;
+}
+
 // s_waitcnt vmcnt(N), the other counters left at their maximum (gfx9 encoding):
 // wait until at most N of this wave's vector-memory operations are outstanding.
 // They complete in issue order, so this waits for all but the N most recent.
@@ -269,6 +275,74 @@ struct DecodeShape {
   int target;         // shared rows: of these, the ones to share the rows of the batch; otherwise 0
   int waves;          // waves per workgroup
   size_t part_bytes;  // partials
+};
+
+// A plan of drafted tokens: of each request its first node and its nodes, and of each node the nodes that it sees
+// (bit j % 32 of word j / 32: node j of its request), `words` words a node.
+constexpr int kMaxNodes = 256;
+struct TreePlan {
+  const int2 *req;
+  const uint32_t *sees;
+  int words;
+};
+
+// The tensors of an attention of drafted tokens (k and v as codes where there are scales).
+struct TreeCall {
+  int batch, total_nodes, max_nodes, max_ctx;
+  TreePlan plan;
+  const void *k, *v;
+  const uint8_t *ks, *vs;
+  const int64_t *row_off;
+  const int32_t *cache_len;
+  const uint16_t *q, *k_new, *v_new;
+  float scale_log2;
+  void *out;
+  bool out_bf16;
+  int32_t *status;
+};
+
+// How such a call is cut into workgroups, and its workspace.
+struct TreeShape {
+  int columns;        // q rows of a workgroup, in blocks of 16
+  int tiles;          // of them in the largest request
+  int splits;         // ranges of a request of max_ctx rows
+  int range;          // 32-row blocks of a range
+  size_t part_bytes;  // partials: [request][kv-head][tile][split] of the values, then of (max, sum)
+};
+
+// The tensors of an append.
+struct AppendCall {
+  int batch, total_new, max_rows;
+  const int32_t *new_cu, *select, *select_len;
+  const uint16_t *k_new, *v_new;
+  void *k, *v;
+  uint8_t *ks, *vs;   // null for bf16 rows
+  const int64_t *row_off;
+  const int32_t *row_cap;
+  int32_t *cache_len;
+  int32_t *status;
+};
+
+constexpr int kMaxVocab = 1 << 28;
+
+// The tensors of a call on logits (null where the program has none).
+struct LogitsCall {
+  int batch, total_rows, max_rows, vocab;
+  bool bf16;
+  const void *logits;
+  TreePlan plan;               // req null: a row a request
+  const int32_t *node_token;
+  const int32_t *tokens;
+  const int64_t *token_off;
+  const int32_t *token_len, *prompt_len;
+  const float *repetition, *presence, *frequency;
+  const int32_t *bias_cu, *bias_token;
+  const float *bias_value;
+  const uint32_t *allowed;
+  float *out;
+  int32_t *best;
+  float *best_value;
+  int32_t *status;
 };
 
 // The decode's fixed-layout scratch (the entry point that allocates nothing): counters

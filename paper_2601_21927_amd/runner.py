@@ -161,6 +161,13 @@ def _evict(cache, keep_head, keep_tail, budget, status, stream, **scales) -> int
     return st
 
 
+def _tree_decode(cache, plan, q, k_new, v_new, out, status, max_nodes, max_ctx, stream, **scales) -> int:
+    n = _bytes(sonic.tree_decode_workspace_bytes, cache.batch, int(max_nodes), q.shape[1], q.shape[2], int(max_ctx))
+    ws = cache.workspaces.get("tree", n, q.device, stream)
+    return sonic.tree_decode(plan, cache.k, cache.v, cache.row_off, cache.length, q, k_new, v_new, out, ws, status, max_nodes, max_ctx,
+                             stream=stream, **scales)
+
+
 class CompactCache:
     """Per-request cache rows [row_off[b], row_off[b] + row_cap[b]) of a [rows, Hkv, d] bf16 pair.
 
@@ -204,6 +211,16 @@ class CompactCache:
         return sonic.compressed_decode_weighted(self.k, self.v, self.row_off, self.row_cap, self.length, q, k_new, v_new, out,
                                                 self.row_weight, ws, status, max_ctx, stream=stream)
 
+    def tree_decode(self, plan, q, k_new, v_new, out, status, max_nodes: int, max_ctx: int, stream=None) -> int:
+        """The attention of drafted tokens over the cache and their own paths; the cache stays as it is."""
+        return _tree_decode(self, plan, q, k_new, v_new, out, status, max_nodes, max_ctx, stream)
+
+    def append(self, new_cu, k_new, v_new, status, max_rows: int, select=None, select_len=None, stream=None) -> int:
+        """New rows to the end of the cache: all of a request's, or those at select.  row_weight and keep_idx of the rows are
+        the caller's to set."""
+        return sonic.cache_append(new_cu, k_new, v_new, self.k, self.v, self.row_off, self.row_cap, self.length, status, max_rows,
+                                  select=select, select_len=select_len, stream=stream)
+
     def evict(self, keep_head, keep_tail, budget, status, stream=None) -> int:
         """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device.  keep_idx
         goes with the rows."""
@@ -245,7 +262,53 @@ class Q4Cache:
         return sonic.cache_expand_q4(self.k, self.k_scale, self.v, self.v_scale, self.row_off, self.row_cap, row_begin, row_end, k,
                                      v, out_row_off, out_row_cap, status, max_rows, stream=stream)
 
+    def tree_decode(self, plan, q, k_new, v_new, out, status, max_nodes: int, max_ctx: int, stream=None) -> int:
+        """The attention of drafted tokens over the cache and their own paths, at the 4-bit values of their rows; the cache
+        stays as it is."""
+        return _tree_decode(self, plan, q, k_new, v_new, out, status, max_nodes, max_ctx, stream, k_scale=self.k_scale,
+                            v_scale=self.v_scale)
+
+    def append(self, new_cu, k_new, v_new, status, max_rows: int, select=None, select_len=None, stream=None) -> int:
+        """New rows, rounded, to the end of the cache: all of a request's, or those at select.  row_weight and keep_idx of the
+        rows are the caller's to set."""
+        return sonic.cache_append(new_cu, k_new, v_new, self.k, self.v, self.row_off, self.row_cap, self.length, status, max_rows,
+                                  select=select, select_len=select_len, k_scale=self.k_scale, v_scale=self.v_scale, stream=stream)
+
     def evict(self, keep_head, keep_tail, budget, status, stream=None) -> int:
         """Drop the rows of least row_weight, in place; keep_head, keep_tail, budget: int32 [B] on the device.  keep_idx
         goes with the rows."""
         return _evict(self, keep_head, keep_tail, budget, status, stream, k_scale=self.k_scale, v_scale=self.v_scale)
+
+
+class DraftStep:
+    """A step over drafted tokens of `batch` requests, up to total_nodes of them and max_nodes a request: what is made once
+    and used by every layer and every step (the plan, the confirmed paths, the logits' workspace).
+
+    plan_trees, then CompactCache.tree_decode (or Q4Cache's) per layer with `plan`, `logits`, `accept`, and the caches'
+    append with path and path_len."""
+
+    def __init__(self, batch: int, total_nodes: int, max_nodes: int, device="cuda"):
+        self.batch, self.total_nodes, self.max_nodes = batch, total_nodes, max_nodes
+
+        def ints(n):
+            return torch.zeros(n, dtype=torch.int32, device=device)
+
+        self.plan = torch.zeros(sonic.tree_plan_bytes(batch, total_nodes, max_nodes), dtype=torch.uint8, device=device)
+        self.path, self.path_len, self.next_token = ints(total_nodes), ints(batch), ints(batch)
+        self.best = ints(total_nodes)
+        self.workspaces = _Workspaces()
+
+    def plan_trees(self, cu_nodes, parent, status, stream=None) -> int:
+        return sonic.tree_plan(cu_nodes, parent, self.total_nodes, self.max_nodes, self.plan, status, stream=stream)
+
+    def logits(self, logits, status, stream=None, **how) -> int:
+        """sonic.logits_process on the nodes' logits [total_nodes, V]: their best tokens to `best`."""
+        n = _bytes(sonic.logits_process_workspace_bytes, *logits.shape)
+        ws = self.workspaces.get("logits", n, logits.device, stream)
+        return sonic.logits_process(logits, self.best, ws, status, plan=self.plan, batch=self.batch, max_nodes=self.max_nodes,
+                                    stream=stream, **how)
+
+    def accept(self, parent, node_token, status, chosen=None, stream=None, **history) -> int:
+        """The nodes that `chosen` (by default the best tokens) confirms, to path, path_len and next_token."""
+        return sonic.tree_accept(self.plan, parent, node_token, self.best if chosen is None else chosen, self.path, self.path_len,
+                                 self.next_token, status, self.max_nodes, stream=stream, **history)

@@ -38,6 +38,8 @@ EXPORTS = (
     "sonic_kv_compact_q4", "sonic_cache_expand_q4", "sonic_decode_q4_workspace_bytes", "sonic_compressed_decode_q4",
     "sonic_decode_weighted_workspace_bytes", "sonic_compressed_decode_weighted", "sonic_kv_compact_weights",
     "sonic_cache_evict_workspace_bytes", "sonic_cache_evict",
+    "sonic_tree_plan_bytes", "sonic_tree_plan", "sonic_tree_decode_workspace_bytes", "sonic_tree_decode",
+    "sonic_logits_process_workspace_bytes", "sonic_logits_process", "sonic_tree_accept", "sonic_cache_append",
 )
 
 _lib = None
@@ -113,6 +115,22 @@ def lib() -> ctypes.CDLL:
     L.sonic_cache_evict_workspace_bytes.argtypes = [_i32] * 2
     L.sonic_cache_evict.restype = _i32
     L.sonic_cache_evict.argtypes = [_i32] * 4 + [_p] * 20 + [_sz, _p, _p]
+    L.sonic_tree_plan_bytes.restype = _sz
+    L.sonic_tree_plan_bytes.argtypes = [_i32] * 3
+    L.sonic_tree_plan.restype = _i32
+    L.sonic_tree_plan.argtypes = [_i32] * 3 + [_p] * 3 + [_sz, _p, _p]
+    L.sonic_tree_decode_workspace_bytes.restype = _sz
+    L.sonic_tree_decode_workspace_bytes.argtypes = [_i32] * 5
+    L.sonic_tree_decode.restype = _i32
+    L.sonic_tree_decode.argtypes = [_i32] * 7 + [_p, _sz] + [_p] * 9 + [_f32, _p, _i32, _p, _sz, _p, _p]
+    L.sonic_logits_process_workspace_bytes.restype = _sz
+    L.sonic_logits_process_workspace_bytes.argtypes = [_i32] * 2
+    L.sonic_logits_process.restype = _i32
+    L.sonic_logits_process.argtypes = [_i32] * 4 + [_p, _i32, _p, _sz] + [_p] * 16 + [_sz, _p, _p]
+    L.sonic_tree_accept.restype = _i32
+    L.sonic_tree_accept.argtypes = [_i32] * 3 + [_p, _sz] + [_p] * 12
+    L.sonic_cache_append.restype = _i32
+    L.sonic_cache_append.argtypes = [_i32] * 5 + [_p] * 14
     _lib = L
     return L
 
@@ -478,3 +496,103 @@ def cache_evict(k_cache, v_cache, cache_row_off, cache_len, row_weight, keep_hea
         ("out_row_cap", out_row_cap, _I32, (B,)), ("out_len", out_len, _I32, (B,)), ("out_weight", out_weight, _F32, (n,)),
         ("keep_idx", keep_idx, _I32, (n,)), ("workspace", workspace, workspace.dtype, None),
         _number(workspace.numel() * workspace.element_size()), ("dev_status", dev_status, _I32, None)])
+
+
+# ----------------------------------------------------------------- a step over drafted tokens
+def _sized(name, t):
+    """A workspace between the tensors of _pass, and its bytes."""
+    return [(name, t, None if t is None else t.dtype, None), _number(0 if t is None else t.numel() * t.element_size())]
+
+
+def tree_plan_bytes(batch: int, total_nodes: int, max_nodes: int) -> int:
+    return int(lib().sonic_tree_plan_bytes(batch, total_nodes, max_nodes))
+
+
+def tree_plan(cu_nodes, parent, total_nodes: int, max_nodes: int, plan, dev_status, stream=None) -> int:
+    """Which nodes every node sees: cu_nodes int32 [B+1]; parent int32 [total_nodes], or None for chains; plan uint8
+    [>= tree_plan_bytes]."""
+    return _pass("tree_plan", lib().sonic_tree_plan, stream, (cu_nodes.numel() - 1, int(total_nodes), int(max_nodes)), [
+        ("cu_nodes", cu_nodes, _I32, None), ("parent", parent, _I32, (total_nodes,)), *_sized("plan", plan),
+        ("dev_status", dev_status, _I32, None)])
+
+
+def tree_decode_workspace_bytes(batch: int, max_nodes: int, num_q_heads: int, head_dim: int, max_ctx: int) -> int:
+    return int(lib().sonic_tree_decode_workspace_bytes(batch, max_nodes, num_q_heads, head_dim, max_ctx))
+
+
+def tree_decode(plan, k_cache, v_cache, cache_row_off, cache_len, q, k_new, v_new, out, workspace, dev_status, max_nodes: int,
+                max_ctx: int, k_scale=None, v_scale=None, softmax_scale=None, stream=None) -> int:
+    """The nodes' attention: q [N,Hq,d] bf16; k_new/v_new [N,Hkv,d] bf16; out [N,Hq,d] fp32 or bf16; a cache of bf16 rows
+    [rows,Hkv,d], or of codes [rows,Hkv,d/2] with k_scale/v_scale [rows,Hkv,d/32]."""
+    N, Hq, d = q.shape
+    Hkv, rows, B = k_new.shape[1], k_cache.shape[0], cache_len.numel()
+    if out.dtype not in (_F32, _BF16):
+        raise TypeError(f"out must be {_F32} or {_BF16}, got {out.dtype}")
+    planes = _planes(rows, Hkv, d, k_cache, k_scale, v_cache, v_scale)
+    scale = 0.0 if softmax_scale is None else float(softmax_scale)   # 0: the library's 1/sqrt(d)
+    return _pass("tree_decode", lib().sonic_tree_decode, stream, (B, N, int(max_nodes), Hq, Hkv, d, int(max_ctx)), [
+        *_sized("plan", plan), *planes, ("cache_row_off", cache_row_off, _I64, (B,)), ("cache_len", cache_len, _I32, None),
+        ("q", q, _BF16, None), ("k_new", k_new, _BF16, (N, Hkv, d)), ("v_new", v_new, _BF16, (N, Hkv, d)), _number(scale),
+        ("out", out, out.dtype, (N, Hq, d)), _number(int(out.dtype is _BF16)), *_sized("workspace", workspace),
+        ("dev_status", dev_status, _I32, None)])
+
+
+def _planes(rows, Hkv, d, k_cache, k_scale, v_cache, v_scale):
+    """A cache's arrays in the order of the C ABI: codes with scales, or bf16 rows with none."""
+    if (k_scale is None) != (v_scale is None):
+        raise ValueError("k_scale and v_scale are given together")
+    if k_scale is not None:
+        return _q4_planes(rows, Hkv, d, k_cache, k_scale, v_cache, v_scale)
+    return [("k_cache", k_cache, _BF16, (rows, Hkv, d)), _number(None), ("v_cache", v_cache, _BF16, (rows, Hkv, d)), _number(None)]
+
+
+def logits_process_workspace_bytes(total_rows: int, vocab: int) -> int:
+    return int(lib().sonic_logits_process_workspace_bytes(total_rows, vocab))
+
+
+def logits_process(logits, best, workspace, dev_status, plan=None, batch=None, max_nodes: int = 1, node_token=None, tokens=None,
+                   token_off=None, token_len=None, prompt_len=None, repetition=None, presence=None, frequency=None, bias_cu=None,
+                   bias_token=None, bias_value=None, allowed=None, best_value=None, out=None, stream=None) -> int:
+    """Penalties, biases and masks on logits [n,V] (fp32 or bf16), and the rows' best tokens: best int32 [n] or None, best_value
+    fp32 [n] or None, out fp32 [n,V] or None.  Rows are the nodes of a plan (of `batch` requests), or one a request.
+    node_token int32 [n]; tokens int32 with token_off int64 [B], token_len and prompt_len int32 [B]; repetition, presence,
+    frequency fp32 [B]; bias_cu int32 [B+1], bias_token int32 and bias_value fp32; allowed int32 [n,(V+31)//32]."""
+    n, V = logits.shape
+    B = int(batch) if batch is not None else n
+    if logits.dtype not in (_F32, _BF16):
+        raise TypeError(f"logits must be {_F32} or {_BF16}, got {logits.dtype}")
+    m = 0 if bias_token is None else bias_token.numel()
+    return _pass("logits_process", lib().sonic_logits_process, stream, (B, n, int(max_nodes), V), [
+        ("logits", logits, logits.dtype, None), _number(int(logits.dtype is _BF16)), *_sized("plan", plan),
+        ("node_token", node_token, _I32, (n,)), ("tokens", tokens, _I32, None), ("token_off", token_off, _I64, (B,)),
+        ("token_len", token_len, _I32, (B,)), ("prompt_len", prompt_len, _I32, (B,)), ("repetition", repetition, _F32, (B,)),
+        ("presence", presence, _F32, (B,)), ("frequency", frequency, _F32, (B,)), ("bias_cu", bias_cu, _I32, (B + 1,)),
+        ("bias_token", bias_token, _I32, None), ("bias_value", bias_value, _F32, (m,)), ("allowed", allowed, _I32, (n, (V + 31) // 32)),
+        ("out", out, _F32, (n, V)), ("best", best, _I32, (n,)), ("best_value", best_value, _F32, (n,)), *_sized("workspace", workspace),
+        ("dev_status", dev_status, _I32, None)])
+
+
+def tree_accept(plan, parent, node_token, chosen, path, path_len, next_token, dev_status, max_nodes: int, tokens=None, token_off=None,
+                token_cap=None, token_len=None, stream=None) -> int:
+    """The nodes that the chosen tokens confirm: parent int32 [N] or None; node_token, chosen, path int32 [N]; path_len,
+    next_token int32 [B]; tokens int32 with token_off int64 [B], token_cap and token_len int32 [B], or none of them."""
+    N, B = node_token.numel(), path_len.numel()
+    return _pass("tree_accept", lib().sonic_tree_accept, stream, (B, N, int(max_nodes)), [
+        *_sized("plan", plan), ("parent", parent, _I32, (N,)), ("node_token", node_token, _I32, None), ("chosen", chosen, _I32, (N,)),
+        ("path", path, _I32, (N,)), ("path_len", path_len, _I32, None), ("next_token", next_token, _I32, (B,)),
+        ("tokens", tokens, _I32, None), ("token_off", token_off, _I64, (B,)), ("token_cap", token_cap, _I32, (B,)),
+        ("token_len", token_len, _I32, (B,)), ("dev_status", dev_status, _I32, None)])
+
+
+def cache_append(new_cu, k_new, v_new, k_cache, v_cache, cache_row_off, cache_row_cap, cache_len, dev_status, max_rows: int, select=None,
+                 select_len=None, k_scale=None, v_scale=None, stream=None) -> int:
+    """New rows k_new/v_new [N,Hkv,d] bf16 to the end of the caches: all of a request's, or those at select int32 [N],
+    select_len int32 [B]; bf16 rows, or codes with scales."""
+    N, Hkv, d = k_new.shape
+    B, rows = new_cu.numel() - 1, k_cache.shape[0]
+    k, ks, v, vs = _planes(rows, Hkv, d, k_cache, k_scale, v_cache, v_scale)
+    return _pass("cache_append", lib().sonic_cache_append, stream, (B, N, int(max_rows), Hkv, d), [
+        ("new_cu", new_cu, _I32, None), ("select", select, _I32, (N,)), ("select_len", select_len, _I32, (B,)),
+        ("k_new", k_new, _BF16, None), ("v_new", v_new, _BF16, (N, Hkv, d)), k, ks, v, vs,
+        ("cache_row_off", cache_row_off, _I64, (B,)), ("cache_row_cap", cache_row_cap, _I32, (B,)),
+        ("cache_len", cache_len, _I32, (B,)), ("dev_status", dev_status, _I32, None)])
