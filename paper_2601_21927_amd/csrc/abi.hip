@@ -66,7 +66,7 @@ hipError_t launch_compact_weights(int batch, int total_tokens, int max_rows, con
 hipError_t launch_evict(const EvictCall &c, const EvictWs &ws, int Hkv, int D, hipStream_t stream);
 hipError_t launch_tree_plan(int batch, int total, int max_nodes, const int32_t *cu, const int32_t *parent, TreePlan plan,
                             int32_t *status, hipStream_t stream);
-TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ctx);
+TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ctx, bool q4);
 hipError_t launch_tree(const TreeCall &c, const TreeShape &sh, float *part, int Hkv, int G, int D, hipStream_t stream);
 hipError_t launch_tree_accept(int batch, int total, int max_nodes, TreePlan plan, const int32_t *parent, const int32_t *node_token,
                               const int32_t *chosen, int32_t *path, int32_t *path_len, int32_t *next_token, int32_t *tokens,
@@ -937,9 +937,10 @@ int32_t sonic_tree_plan(int32_t batch, int32_t total_nodes, int32_t max_nodes, c
 
 size_t sonic_tree_decode_workspace_bytes(int32_t batch, int32_t max_nodes, int32_t Hq, int32_t d, int32_t max_ctx) {
   if (batch <= 0 || max_nodes <= 0 || Hq <= 0 || max_ctx < 0) return 256;
-  size_t part = 0;   // for any kv-head count the call may use
+  size_t part = 0;   // for any kv-head count the call may use, and either kind of rows
   for (int hkv = 1; hkv <= Hq; ++hkv)
-    if (Hq % hkv == 0 && Hq / hkv <= 8) part = std::max(part, tree_shape(batch, hkv, Hq / hkv, d, max_nodes, max_ctx).part_bytes);
+    for (bool q4 : {false, true})
+      if (Hq % hkv == 0 && Hq / hkv <= 8) part = std::max(part, tree_shape(batch, hkv, Hq / hkv, d, max_nodes, max_ctx, q4).part_bytes);
   return align_up(part + 256, 256);
 }
 
@@ -963,7 +964,7 @@ int32_t sonic_tree_decode(int32_t batch, int32_t total_nodes, int32_t max_nodes,
   if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4) || !aligned(q, 16) ||
       !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(out, 16) || !aligned(workspace, 256))
     return SONIC_ERR_INVALID_ARG;
-  const TreeShape sh = tree_shape(batch, Hkv, Hq / Hkv, d, max_nodes, max_ctx);
+  const TreeShape sh = tree_shape(batch, Hkv, Hq / Hkv, d, max_nodes, max_ctx, k_scale != nullptr);
   if (workspace_bytes < sh.part_bytes) return SONIC_ERR_WORKSPACE;
   if ((static_cast<long>(batch) * Hkv * sh.splits + kNumXcd) * sh.tiles > INT32_MAX) return SONIC_ERR_UNSUPPORTED;   // the grid
   TreeCall c{};

@@ -304,9 +304,11 @@ struct TreeCall {
 // How such a call is cut into workgroups, and its workspace.
 struct TreeShape {
   int columns;        // q rows of a workgroup, in blocks of 16
+  int waves;          // of a workgroup of up to 32 rows
   int tiles;          // of them in the largest request
   int splits;         // ranges of a request of max_ctx rows
   int range;          // 32-row blocks of a range
+  int groups;         // threads that share a row's ranges when they are joined
   size_t part_bytes;  // partials: [request][kv-head][tile][split] of the values, then of (max, sum)
 };
 
