@@ -7,9 +7,14 @@
 // every operation rounded to fp32 by itself, so that a best token does not depend on how the compiler joins them.
 //
 // logits_kernel: a workgroup has a piece of the vocabulary and some rows of one request.  It counts the request's tokens
-// that fall into the piece in LDS, a word per token (count, seen, biased), once for its rows; per row the path's tokens are
-// added and taken off again.  The row is then one pass over its logits, 16 bytes a lane; nearly all words are zero and cost
-// a compare.  Bound by the bytes of the logits.  logits_best_kernel picks each row's best from the pieces' and raises errors.
+// that fall into the piece in LDS, a word per token (count, seen, biased) and a bit per token that has one, once for its
+// rows; per row the path's tokens are added and taken off again.  A row is then one pass over its logits, 16 bytes a lane,
+// in which a thread's tokens that have a word are mended one after the other: there are few, but most waves have some
+// among any 256 tokens, and did the penalties' divisions for all of them (256 rows of 128,000 in bf16, written out: 73 us
+// so, 62 this way).  The next row's logits, mask words and path are requested ahead of this row's stores, so that a row
+// waits for nothing of its own (55 us; 201 MB, 3.7 TB/s).  Where rows are few, a chain of loads is what counts: lengths, then
+// history and logits, then biases (64 rows of 150,001 with histories of up to 9,000 tokens, 41 MB: 26 us).
+// logits_best_kernel picks each row's best from the pieces' and raises errors.
 #include <algorithm>
 
 #include "common.h"
@@ -54,74 +59,33 @@ __device__ __forceinline__ bool logits_request(const LogitsCall &c, int b, Logit
   return !bad;
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int group, int pieces, Best *__restrict__ part) {
-  constexpr int PE = BF16 ? 8 : 4;             // elements of 16 bytes
-  constexpr int STEPS = (kPiece + PE) / (PE * kLogitThreads) + 1;
-  __shared__ __align__(16) uint32_t s_word[kPiece];
-  __shared__ int s_entry[kPiece];              // the token's bias, as an entry of the request's
-  __shared__ Best s_best[kLogitThreads / kWave];
-  __shared__ int s_stop;
-  const int b = blockIdx.z, t0 = blockIdx.x * kPiece, t1 = min(c.vocab, t0 + kPiece);
-  LogitsReq r;
-  const bool good = logits_request(c, b, &r);
-  if (threadIdx.x == 0) s_stop = step_stops(c.status);
-  __syncthreads();
-  const int row0 = blockIdx.y * group, row1 = min(r.rows, row0 + group);
-  if (!good || row0 >= row1) return;
-  if (s_stop) {   // other workgroups of the call may have seen no error: no best is made of this piece and theirs
-    for (int row = row0 + threadIdx.x; row < row1; row += kLogitThreads)
-      part[static_cast<size_t>(r.first + row) * pieces + blockIdx.x] = Best{0.f, kStopped};
-    return;
-  }
+// The 16-byte parts of a row that a thread has: part k is tokens first + PE (thread + k * threads) .. + PE - 1.
+// What else a row needs of memory comes along: the words of its mask, and of the nodes that it sees.
+template <bool BF16> struct RowParts {
+  static constexpr int PE = BF16 ? 8 : 4;      // elements of 16 bytes
+  static constexpr int STEPS = (kPiece + PE) / (PE * kLogitThreads) + 1;
+  u32x4 raw[STEPS];
+  uint32_t low[STEPS], high[STEPS];            // of the mask: the words from a part's first token on
+  uint32_t sees;
 
-  for (int i = threadIdx.x; i < kPiece; i += kLogitThreads) {
-    s_word[i] = 0;
-    s_entry[i] = -1;
-  }
-  __syncthreads();
-  auto in_piece = [&](int t) { return t >= t0 && t < t1; };
-  for (int i = threadIdx.x; i < r.len; i += kLogitThreads) {
-    const int t = c.tokens[r.off + i];
-    if (in_piece(t)) {
-      if (i < r.prompt) atomicOr(&s_word[t - t0], kSeen);
-      else atomicAdd(&s_word[t - t0], 1u);
-    }
-  }
-  for (int i = threadIdx.x; i < r.biases; i += kLogitThreads) {
-    const int t = c.bias_token[r.bias0 + i];
-    if (in_piece(t)) {
-      atomicOr(&s_word[t - t0], kBiased);
-      atomicMax(&s_entry[t - t0], i);           // of several entries for a token the last one counts
-    }
-  }
-  const float rep = c.repetition != nullptr ? c.repetition[b] : 1.f;
-  const float presence = c.presence != nullptr ? c.presence[b] : 0.f, frequency = c.frequency != nullptr ? c.frequency[b] : 0.f;
-  __syncthreads();
+  // First token of the parts: the piece starts up to PE - 1 tokens behind a 16-byte border.
+  __device__ __forceinline__ static int first(size_t start, int t0) { return t0 - static_cast<int>((start + t0) % PE); }
 
-  for (int row = row0; row < row1; ++row) {
-    const size_t at = static_cast<size_t>(r.first + row);
-    // the path's tokens: thread j has node j
-    int mine = -1;
-    if (c.node_token != nullptr) {
-      const int j = threadIdx.x;
-      if (c.plan.req == nullptr) {
-        if (j == 0) mine = c.node_token[at];
-      } else if (j < r.rows && ((c.plan.sees[at * c.plan.words + j / 32] >> (j % 32)) & 1)) {
-        mine = c.node_token[r.first + j];
-      }
-      if (in_piece(mine)) atomicAdd(&s_word[mine - t0], 1u);
-      __syncthreads();
-    }
+  __device__ __forceinline__ void load(const LogitsCall &c, size_t at, int t0, int t1) {
     const size_t start = at * c.vocab;
-    const int skew = static_cast<int>((start + t0) % PE);   // the piece starts that far behind a 16-byte border
-    const uint32_t *allowed = c.allowed != nullptr ? c.allowed + at * ((c.vocab + 31) / 32) : nullptr;
-    u32x4 raw[STEPS];
+    const int f = first(start, t0), mask_words = (c.vocab + 31) / 32;
+    sees = c.plan.req != nullptr && static_cast<int>(threadIdx.x) < c.max_rows ? c.plan.sees[at * c.plan.words + threadIdx.x / 32] : 0;
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
-      const int t = t0 - skew + PE * (static_cast<int>(threadIdx.x) + k * kLogitThreads);
+      const int t = f + PE * (static_cast<int>(threadIdx.x) + k * kLogitThreads);
       raw[k] = u32x4{0, 0, 0, 0};
+      low[k] = high[k] = ~0u;
       if (t >= t1) continue;
+      if (c.allowed != nullptr) {
+        const uint32_t *allowed = c.allowed + at * mask_words + max(t, 0) / 32;
+        low[k] = allowed[0];
+        high[k] = allowed[max(t, 0) / 32 + 1 < mask_words ? 1 : 0];
+      }
       if (t >= 0 && t + PE <= c.vocab) {
         raw[k] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(c.logits) + (start + t) * (BF16 ? 2 : 4));
       } else {   // the row's ends
@@ -133,66 +97,180 @@ __global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int
         }
       }
     }
-    Best best{-INFINITY, -1};
+  }
+};
+
+// Bits t .. of a bit array whose words t / 32 and one on are low and high; t from -PE + 1 on, low its first word then.
+__device__ __forceinline__ uint32_t bits_from(uint32_t low, uint32_t high, int t) {
+  return t < 0 ? low << -t : __builtin_amdgcn_alignbit(high, low, t % 32);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int group, int pieces, Best *__restrict__ part) {
+  typedef RowParts<BF16> Parts;
+  constexpr int PE = Parts::PE, STEPS = Parts::STEPS, AHEAD = 8, WORDS = kPiece / 32;
+  __shared__ __align__(16) uint32_t s_word[kPiece];
+  __shared__ int s_entry[kPiece];              // the token's bias, as an entry of the request's
+  __shared__ uint32_t s_has[WORDS];            // tokens that have a word
+  __shared__ float s_max[kLogitThreads / kWave];
+  __shared__ int s_token, s_stop;
+  const int b = blockIdx.z, t0 = blockIdx.x * kPiece, t1 = min(c.vocab, t0 + kPiece);
+  LogitsReq r;
+  const bool good = logits_request(c, b, &r);
+  if (threadIdx.x == 0) {
+    s_stop = step_stops(c.status);
+    s_token = INT32_MAX;
+  }
+  for (int i = threadIdx.x; i < kPiece / 4; i += kLogitThreads) reinterpret_cast<u32x4 *>(s_word)[i] = u32x4{0, 0, 0, 0};
+  if (threadIdx.x < WORDS) s_has[threadIdx.x] = 0;
+  lds_barrier();
+  const int row0 = blockIdx.y * group, row1 = min(r.rows, row0 + group);
+  if (!good || row0 >= row1) return;
+  if (s_stop) {   // other workgroups of the call may have seen no error: no best is made of this piece and theirs
+    for (int row = row0 + threadIdx.x; row < row1; row += kLogitThreads)
+      part[static_cast<size_t>(r.first + row) * pieces + blockIdx.x] = Best{0.f, kStopped};
+    return;
+  }
+
+  // the first row's logits are on their way while the history is counted
+  Parts x;
+  x.load(c, r.first + row0, t0, t1);
+  auto in_piece = [&](int t) { return t >= t0 && t < t1; };
+  auto has = [&](int i) { atomicOr(&s_has[i / 32], 1u << (i % 32)); };
+  // thread j has node j of the request, whose token the rows that see it count
+  int token = -1;
+  if (c.node_token != nullptr && c.plan.req != nullptr && static_cast<int>(threadIdx.x) < r.rows) token = c.node_token[r.first + threadIdx.x];
+  for (int i0 = threadIdx.x; i0 < r.len; i0 += AHEAD * kLogitThreads) {
+    int t[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + k * kLogitThreads;
+      t[k] = i < r.len ? c.tokens[r.off + i] : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (in_piece(t[k])) {
+        if (i0 + k * kLogitThreads < r.prompt) atomicOr(&s_word[t[k] - t0], kSeen);
+        else atomicAdd(&s_word[t[k] - t0], 1u);
+        has(t[k] - t0);
+      }
+  }
+  if (r.biases > 0) {
+    for (int i = threadIdx.x; i < r.biases; i += kLogitThreads) {   // (few tokens of the piece have one: theirs start at -1)
+      const int t = c.bias_token[r.bias0 + i];
+      if (in_piece(t)) {
+        atomicOr(&s_word[t - t0], kBiased);
+        has(t - t0);
+        s_entry[t - t0] = -1;
+      }
+    }
+    lds_barrier();
+    for (int i = threadIdx.x; i < r.biases; i += kLogitThreads) {
+      const int t = c.bias_token[r.bias0 + i];
+      if (in_piece(t)) atomicMax(&s_entry[t - t0], i);              // of several entries for a token the last one counts
+    }
+  }
+  const float rep = c.repetition != nullptr ? c.repetition[b] : 1.f;
+  const float presence = c.presence != nullptr ? c.presence[b] : 0.f, frequency = c.frequency != nullptr ? c.frequency[b] : 0.f;
+  lds_barrier();
+
+  for (int row = row0; row < row1; ++row) {
+    const size_t at = static_cast<size_t>(r.first + row), start = at * c.vocab;
+    // the path's tokens
+    int mine = -1;
+    if (c.node_token != nullptr) {
+      const int j = threadIdx.x;
+      if (c.plan.req == nullptr) {
+        if (j == 0) mine = c.node_token[at];
+      } else if (j < r.rows && ((x.sees >> (j % 32)) & 1)) {
+        mine = token;
+      }
+      if (in_piece(mine)) {
+        atomicAdd(&s_word[mine - t0], 1u);
+        has(mine - t0);
+      }
+      lds_barrier();
+    }
+    const int f = Parts::first(start, t0) + PE * static_cast<int>(threadIdx.x);   // the thread's first token
+    float v[STEPS][PE], top = -INFINITY;
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
-      const int t = t0 - skew + PE * (static_cast<int>(threadIdx.x) + k * kLogitThreads);
+      const int t = f + k * PE * kLogitThreads;
+#pragma unroll
+      for (int e = 0; e < PE; ++e) v[k][e] = -INFINITY;
       if (t >= t1) continue;
-      uint32_t bits = ~0u;
-      if (allowed != nullptr) {
-        const int w0 = max(t, 0) / 32, w1 = min(t + PE - 1, c.vocab - 1) / 32;
-        const uint64_t both = static_cast<uint64_t>(allowed[w1]) << 32 | allowed[w0];
-        bits = static_cast<uint32_t>(t < 0 ? both << -t : w1 > w0 ? both >> (t % 32) : (both & 0xFFFFFFFFu) >> (t % 32));
-      }
-      float x[PE];
+      uint32_t in = (1u << PE) - 1;            // tokens of the piece
+      if (t < t0) in &= ~0u << (t0 - t);
+      if (t + PE > t1) in &= ~(~0u << (t1 - t));
+      uint32_t ok = in;
+      ok &= bits_from(x.low[k], x.high[k], t);   // (all ones without a mask)
 #pragma unroll
       for (int e = 0; e < PE; ++e) {
-        if constexpr (BF16) x[e] = e & 1 ? bf16_hi(raw[k][e / 2]) : bf16_lo(raw[k][e / 2]);
-        else x[e] = __uint_as_float(raw[k][e]);
-        const bool in = t + e >= t0 && t + e < t1;
-        const uint32_t word = s_word[in ? t + e - t0 : 0];
-        if (in && word != 0) {
-          if (word & (kSeen | kCount)) x[e] = x[e] > 0.f ? x[e] / rep : x[e] * rep;
-          if (word & kCount) {
-            const float off = frequency * static_cast<float>(word & kCount);
-            x[e] = x[e] - (presence + off);
-          }
-          if (word & kBiased) x[e] = x[e] + c.bias_value[r.bias0 + s_entry[t + e - t0]];
-        }
-        if (((bits >> e) & 1) == 0) x[e] = -INFINITY;
-        if (in && x[e] > best.value) best = Best{x[e], t + e};
+        if constexpr (BF16) v[k][e] = e & 1 ? bf16_hi(x.raw[k][e / 2]) : bf16_lo(x.raw[k][e / 2]);
+        else v[k][e] = __uint_as_float(x.raw[k][e]);
       }
-      if (c.out != nullptr) {
+      for (uint32_t left = bits_from(s_has[max(t - t0, 0) / 32], s_has[min(max(t - t0, 0) / 32 + 1, WORDS - 1)], t - t0) & ok; left != 0; left &= left - 1) {
+        const int e = __builtin_ctz(left);
+        const uint32_t word = s_word[t + e - t0];
+        float y = v[k][0];
+#pragma unroll
+        for (int i = 1; i < PE; ++i) y = e == i ? v[k][i] : y;
+        if (word & (kSeen | kCount)) y = y > 0.f ? y / rep : y * rep;
+        if (word & kCount) {
+          const float off = frequency * static_cast<float>(word & kCount);
+          y = y - (presence + off);
+        }
+        if (word & kBiased) y = y + c.bias_value[r.bias0 + s_entry[t + e - t0]];
+#pragma unroll
+        for (int i = 0; i < PE; ++i) v[k][i] = e == i ? y : v[k][i];
+      }
+#pragma unroll
+      for (int e = 0; e < PE; ++e) {
+        v[k][e] = (ok >> e) & 1 ? v[k][e] : -INFINITY;
+        top = fmaxf(top, v[k][e]);
+      }
+    }
+    if (row + 1 < row1) x.load(c, at + 1, t0, t1);   // on their way (ahead of the stores) while the rest is done
+    if (c.out != nullptr) {
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) {
+        const int t = f + k * PE * kLogitThreads;
         float *o = c.out + start + t;
         if (t >= t0 && t + PE <= t1) {
 #pragma unroll
-          for (int e = 0; e < PE; e += 4) *reinterpret_cast<f32x4 *>(o + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+          for (int e = 0; e < PE; e += 4) *reinterpret_cast<f32x4 *>(o + e) = f32x4{v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3]};
         } else {
 #pragma unroll
           for (int e = 0; e < PE; ++e)
-            if (t + e >= t0 && t + e < t1) o[e] = x[e];
+            if (t + e >= t0 && t + e < t1) o[e] = v[k][e];
         }
       }
     }
-    // the piece's best: a thread's tokens ascend, so the greatest value's first is its lowest; between threads the lower token
+    // the piece's greatest value (a NaN is passed over), then the lowest token that has it
+    float most = top;
 #pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-      const float v = __shfl_xor(best.value, o);
-      const int t = __shfl_xor(best.token, o);
-      if (t >= 0 && (v > best.value || (v == best.value && t < best.token))) best = Best{v, t};
-    }
-    if (threadIdx.x % kWave == 0) s_best[threadIdx.x / kWave] = best;
-    __syncthreads();
-    if (in_piece(mine)) atomicSub(&s_word[mine - t0], 1u);
-    if (threadIdx.x == 0) {
+    for (int o = kWave / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    if (threadIdx.x % kWave == 0) s_max[threadIdx.x / kWave] = most;
+    lds_barrier();
+    if (in_piece(mine) && atomicSub(&s_word[mine - t0], 1u) == 1) atomicAnd(&s_has[(mine - t0) / 32], ~(1u << ((mine - t0) % 32)));
 #pragma unroll
-      for (int w = 1; w < kLogitThreads / kWave; ++w) {
-        const Best o = s_best[w];
-        if (o.token >= 0 && (o.value > best.value || (o.value == best.value && o.token < best.token))) best = o;
+    for (int w = 0; w < kLogitThreads / kWave; ++w) most = fmaxf(most, s_max[w]);
+    if (most > -INFINITY) {
+      if (top == most) {
+        int lowest = INT32_MAX;
+#pragma unroll
+        for (int k = STEPS - 1; k >= 0; --k)
+#pragma unroll
+          for (int e = PE - 1; e >= 0; --e)
+            if (v[k][e] == most) lowest = f + k * PE * kLogitThreads + e;
+        atomicMin(&s_token, lowest);
       }
-      part[at * pieces + blockIdx.x] = best;
     }
-    __syncthreads();
+    lds_barrier();
+    if (threadIdx.x == 0) {
+      part[at * pieces + blockIdx.x] = Best{most, most > -INFINITY ? s_token : -1};
+      s_token = INT32_MAX;                     // (the next row's are behind a barrier)
+    }
   }
 }
 
