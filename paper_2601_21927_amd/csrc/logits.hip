@@ -132,21 +132,26 @@ __global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int
     return;
   }
 
-  // the first row's logits are on their way while the history is counted
-  Parts x;
-  x.load(c, r.first + row0, t0, t1);
   auto in_piece = [&](int t) { return t >= t0 && t < t1; };
   auto has = [&](int i) { atomicOr(&s_has[i / 32], 1u << (i % 32)); };
   // thread j has node j of the request, whose token the rows that see it count
   int token = -1;
   if (c.node_token != nullptr && c.plan.req != nullptr && static_cast<int>(threadIdx.x) < r.rows) token = c.node_token[r.first + threadIdx.x];
-  for (int i0 = threadIdx.x; i0 < r.len; i0 += AHEAD * kLogitThreads) {
-    int t[AHEAD];
+  int t[AHEAD];
+  auto request = [&](int i0) {
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       const int i = i0 + k * kLogitThreads;
       t[k] = i < r.len ? c.tokens[r.off + i] : -1;
     }
+  };
+  // the first tokens of the history, the first biases and the first row are on their way together
+  request(threadIdx.x);
+  const int bias = static_cast<int>(threadIdx.x) < r.biases ? c.bias_token[r.bias0 + threadIdx.x] : -1;
+  Parts x;
+  x.load(c, r.first + row0, t0, t1);
+  for (int i0 = threadIdx.x; i0 < r.len; i0 += AHEAD * kLogitThreads) {
+    if (i0 >= AHEAD * kLogitThreads) request(i0);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k)
       if (in_piece(t[k])) {
@@ -157,7 +162,7 @@ __global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int
   }
   if (r.biases > 0) {
     for (int i = threadIdx.x; i < r.biases; i += kLogitThreads) {   // (few tokens of the piece have one: theirs start at -1)
-      const int t = c.bias_token[r.bias0 + i];
+      const int t = i < kLogitThreads ? bias : c.bias_token[r.bias0 + i];
       if (in_piece(t)) {
         atomicOr(&s_word[t - t0], kBiased);
         has(t - t0);
@@ -166,7 +171,7 @@ __global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int
     }
     lds_barrier();
     for (int i = threadIdx.x; i < r.biases; i += kLogitThreads) {
-      const int t = c.bias_token[r.bias0 + i];
+      const int t = i < kLogitThreads ? bias : c.bias_token[r.bias0 + i];
       if (in_piece(t)) atomicMax(&s_entry[t - t0], i);              // of several entries for a token the last one counts
     }
   }

@@ -730,25 +730,25 @@ again:
   }
 }
 
-// More than 32 q rows: RW waves with 32 of them each share the blocks in LDS, KW = 4 / RW such groups take the two blocks of
-// a 64-row step between them.  While a step is computed the next rows stream into the other buffers: K of step c + 2 once
+// More than 32 q rows: RW waves with 32 of them each share the blocks in LDS, KW = NW / RW such groups take the NW / 2 blocks of
+// a step between them.  While a step is computed the next rows stream into the other buffers: K of step c + 2 once
 // every wave has taken its scores of step c, V of step c + 1 once every wave is done with that of c - 1.  Each wave issues
 // NJ direct-to-LDS loads per tensor and step, in the order K(0) V(0) K(1) | V(1) K(2) | .., also past the end (there the last
 // block again), so at either wait all but the 2 NJ most recent are what is waited for.  4-bit rows are decoded on the way:
 // the codes of a step ahead wait in registers, one quantisation block a lane.
-template <int D, int RW, bool Q4, int PARTS>
-__global__ __launch_bounds__(kTreeWaves *kWave, 2) void tree_wide_kernel(TreeCall c, TreeShape sh, float *__restrict__ part, int Hkv, int G) {
+template <int D, int RW, int NW, bool Q4, int PARTS>
+__global__ __launch_bounds__(NW *kWave, 2) void tree_wide_kernel(TreeCall c, TreeShape sh, float *__restrict__ part, int Hkv, int G) {
   typedef TreeColumns<D, 2, PARTS> Columns;
   constexpr int CT = 2, KS = D / 32, DB = D / 16, DC = D / 8, BR = kTreeBlock;
-  constexpr int KW = kTreeWaves / RW, NB = 2 / KW;   // key groups; blocks of a step that a wave takes
+  constexpr int KW = NW / RW, SB = NW / 2, NB = SB / KW;   // key groups; blocks of a step, and of them a wave's
   constexpr int NI = BR * DC / kWave;                // direct-to-LDS instructions per tensor and block
-  constexpr int NJ = 2 * NI / kTreeWaves;            // ... and of a wave per tensor and step
+  constexpr int NJ = SB * NI / NW;                   // ... and of a wave per tensor and step
   constexpr int COLS = 32 * RW;
   constexpr int TILE = BR * D;
-  static_assert(NB * KW == 2 && NI % NJ == 0, "a step is two blocks; a wave loads from one of them");
-  static_assert(kTreeWaves * CT * DB * kWave * 8 <= 8 * TILE, "the join fits");
-  __shared__ __align__(16) uint16_t lds[8 * TILE];   // K of two steps, V of two steps
-  __shared__ float2 stat[kTreeWaves * 32];
+  static_assert(NB * KW == SB && NI % NJ == 0, "a step is whole blocks; a wave loads from one of them");
+  static_assert(NW * CT * DB * kWave * 8 <= 4 * SB * TILE, "the join fits");
+  __shared__ __align__(16) uint16_t lds[4 * SB * TILE];   // K of two steps, V of two steps
+  __shared__ float2 stat[NW * 32];
   TreePlace p;
   if (!tree_begin<D, COLS>(c, sh, part, Hkv, G, &p)) return;
   const TreeReq &r = p.r;
@@ -765,15 +765,15 @@ __global__ __launch_bounds__(kTreeWaves *kWave, 2) void tree_wide_kernel(TreeCal
   const size_t row_elems = static_cast<size_t>(Hkv) * D;
   const uint16_t *knew = c.k_new + static_cast<size_t>(r.first) * row_elems + kvh * D;
   const uint16_t *vnew = c.v_new + static_cast<size_t>(r.first) * row_elems + kvh * D;
-  uint16_t *const kbuf = lds, *const vbuf = lds + 4 * TILE;   // [2 steps][2 blocks][32 rows][D]
-  const int steps = (p.last - first + 1) / 2;
+  uint16_t *const kbuf = lds, *const vbuf = lds + 2 * SB * TILE;   // [2 steps][SB blocks][32 rows][D]
+  const int steps = (p.last - first + SB - 1) / SB;
   const int full = r.len / BR;                       // blocks without a row that some column does not see
   bool careful = false, odd = false;
 
   // One step: `between` runs behind the scores (the V of the step is there when it returns).
   auto compute = [&](int step, auto between) {
-    const uint16_t *kt = kbuf + (step & 1) * 2 * TILE;
-    uint16_t *vt = vbuf + (step & 1) * 2 * TILE;
+    const uint16_t *kt = kbuf + (step & 1) * SB * TILE;
+    uint16_t *vt = vbuf + (step & 1) * SB * TILE;
     f32x4 s[NB][CT][2];
     if (!rowless) {
 #pragma unroll
@@ -782,7 +782,7 @@ __global__ __launch_bounds__(kTreeWaves *kWave, 2) void tree_wide_kernel(TreeCal
     }
     between();
     if (rowless) return;
-    const int g = first + 2 * step + kg;
+    const int g = first + SB * step + kg;
     if (__builtin_expect(g + KW * (NB - 1) >= full, 0))
 #pragma unroll
       for (int n = 0; n < NB; ++n) tree_mask<CT>(c, r, g + KW * n, cached, node, quarter, s[n]);
@@ -806,7 +806,7 @@ again:
     const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint16_t *)lds)) +
                         wave * NJ * kWave * 16;
     auto issue = [&](int step, const uint16_t *cache, const uint16_t *fresh, uint32_t to, bool is_v) {
-      const int g = min(first + 2 * step + wave * NJ / NI, blocks - 1);
+      const int g = min(first + SB * step + wave * NJ / NI, blocks - 1);
       const int r0 = (g < cached ? g : g - cached) * BR;
       const int left = (g < cached ? r.len : r.nodes) - r0;
       const char *src = reinterpret_cast<const char *>(g < cached ? cache : fresh) + static_cast<size_t>(r0) * row_bytes;
@@ -814,11 +814,11 @@ again:
       for (int i = 0; i < NJ; ++i) {
         const int rl = ((wave * NJ % NI + i) * kWave + lane) / DC, pos = lane % DC;
         dma_row16_s(src, min(rl, left - 1) * row_bytes + (pos ^ (is_v ? 2 * (rl & Columns::VSWZ) : rl & Columns::KSWZ)) * 16,
-                    to + (step & 1) * (4 * TILE) + i * kWave * 16);
+                    to + (step & 1) * (2 * SB * TILE) + i * kWave * 16);
       }
     };
     auto issue_k = [&](int step) { issue(step, kbase, knew, at, false); };
-    auto issue_v = [&](int step) { issue(step, vbase, vnew, at + 8 * TILE, true); };
+    auto issue_v = [&](int step) { issue(step, vbase, vnew, at + 4 * SB * TILE, true); };
     issue_k(0);
     issue_v(0);
     issue_k(1);
@@ -837,14 +837,14 @@ again:
   } else {
     constexpr int LV = D / kQ4Block, HALF = D == 64 ? 2 : 1;   // a lane has a block of K and one of V, or (d = 64) one of either
     const size_t row_codes = static_cast<size_t>(Hkv) * (D / 2), row_scales = static_cast<size_t>(Hkv) * LV;
-    const int item = threadIdx.x % (kTreeWaves * kWave / HALF), row = item / LV, blk = item % LV;
-    const bool does_v = HALF == 1 || threadIdx.x >= kTreeWaves * kWave / 2;
+    const int item = threadIdx.x % (NW * kWave / HALF), row = item / LV, blk = item % LV;
+    const bool does_v = HALF == 1 || threadIdx.x >= NW * kWave / 2;
     const size_t code0 = static_cast<size_t>(r.base) * row_codes + kvh * (D / 2) + 16 * blk;
     const size_t scale0 = static_cast<size_t>(r.base) * row_scales + kvh * LV + blk;
     struct Raw { u32x4 c; uint32_t s; };
     auto fetch = [&](int step, const void *codes, const uint8_t *scales, const uint16_t *fresh) {
       Raw x;
-      const int g = min(first + 2 * step + row / BR, blocks - 1);
+      const int g = min(first + SB * step + row / BR, blocks - 1);
       if (g < cached) {
         const size_t at = min(g * BR + row % BR, r.len - 1);
         x.c = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(codes) + code0 + at * row_codes);
@@ -874,13 +874,13 @@ again:
       if (HALF == 1 || !does_v) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<bf16x8 *>(kbuf + (step & 1) * 2 * TILE + row * D + ((4 * blk + i) ^ (row & Columns::KSWZ)) * 8) =
+          *reinterpret_cast<bf16x8 *>(kbuf + (step & 1) * SB * TILE + row * D + ((4 * blk + i) ^ (row & Columns::KSWZ)) * 8) =
               q4_decode8(kq.c[i], q4_scale(kq.s));
       }
       if (does_v) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<bf16x8 *>(vbuf + (step & 1) * 2 * TILE + row * D + ((2 * blk + i / 2) ^ (row & Columns::VSWZ)) * 16 + (i & 1) * 8) =
+          *reinterpret_cast<bf16x8 *>(vbuf + (step & 1) * SB * TILE + row * D + ((2 * blk + i / 2) ^ (row & Columns::VSWZ)) * 16 + (i & 1) * 8) =
               q4_decode8(vq.c[i], q4_scale(vq.s));
       }
     };
@@ -992,9 +992,10 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeCall c, Tre
 //   of 8,000 rows, trees of 16: 4 ranges 20.8 us, 8 16.1, 16 18.0; 8 of 1,328 rows, trees of 8: one range 14.7, two 16.1.
 //   Uneven lengths are not evened out: 64 requests of 180 .. 4,300 rows, trees of up to 16, took 114 us in one range each, 106 to
 //   109 in three or in ranges shared evenly over the batch, which cost 64 equal ones of 1,500 rows 85 us instead of 77.
-// - Eight waves for a tile of up to 32 rows where a CU has one workgroup and that is long: the same waves for fewer ranges
-//   (4 requests of 7,552 rows, 28 / 4 heads, trees of 61, fp32: 67 us, with four 73; one of 100,001 4-bit rows: 16 ranges of
-//   eight waves 73, 32 of four 74, and 16 of four 99).
+// - Eight waves where a CU has one workgroup: of up to 32 rows if it is long (4 requests of 7,552 rows, 28 / 4 heads, trees of
+//   61, fp32: 67 us, with four 73; one of 100,001 4-bit rows: 16 ranges of eight waves 73, 32 of four 74, and 16 of four 99),
+//   of more rows always (chains of 250 over four requests of 1,584 rows 42.6 and 49.9; trees of 64 over eight of 1,328 24.5
+//   and 27.6).  With two workgroups a CU four are better (64 requests of 1,500 rows, trees of 16: 78, with eight 84).
 TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ctx, bool q4) {
   TreeShape sh{};
   const long rows = static_cast<long>(max_nodes) * G, pairs = static_cast<long>(batch) * Hkv;
@@ -1005,9 +1006,9 @@ TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ct
   sh.tiles = static_cast<int>(tiles(sh.columns));
   const long units = pairs * sh.tiles;
   const long splits = std::max(1L, std::min(256 / units, blocks / (units >= 128 ? 32 : 16)));
-  sh.range = static_cast<int>((blocks + splits - 1) / splits + 1) / 2 * 2;   // whole 64-row steps
+  sh.range = static_cast<int>((blocks + splits - 1) / splits + 3) / 4 * 4;   // whole steps
   sh.splits = static_cast<int>((blocks + sh.range - 1) / sh.range);
-  sh.waves = sh.columns <= 2 && units * sh.splits <= 256 && sh.range > (q4 ? 32 : 96) ? 8 : 4;
+  sh.waves = units * sh.splits <= 256 && (sh.columns > 2 || sh.range > (q4 ? 32 : 96)) ? 8 : 4;
   for (sh.groups = 1; sh.groups < 8 && sh.groups * kJoinAhead < sh.splits; sh.groups *= 2) {}
   sh.part_bytes = sh.splits > 1 ? static_cast<size_t>(units) * sh.splits * 16 * sh.columns * (D + 2) * sizeof(float) : 0;
   return sh;
@@ -1020,8 +1021,10 @@ static void launch_tree_rows(const TreeCall &c, const TreeShape &sh, float *part
   else if (sh.columns == 1) tree_kernel<D, 1, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
   else if (sh.columns == 2 && sh.waves == 8) tree_kernel<D, 2, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, part, Hkv, G);
   else if (sh.columns == 2) tree_kernel<D, 2, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
-  else if (sh.columns == 4) tree_wide_kernel<D, 2, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
-  else tree_wide_kernel<D, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
+  else if (sh.columns == 4 && sh.waves == 8) tree_wide_kernel<D, 2, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, part, Hkv, G);
+  else if (sh.columns == 4) tree_wide_kernel<D, 2, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
+  else if (sh.waves == 8) tree_wide_kernel<D, 4, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, part, Hkv, G);
+  else tree_wide_kernel<D, 4, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
 }
 
 template <int D>
