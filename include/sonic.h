@@ -658,7 +658,7 @@ size_t sonic_tree_decode_workspace_bytes(int32_t batch, int32_t max_nodes, int32
  *     out[i][h] = softmax_r(scale * <q[i][h], k[r][g(h)]>) v[r][g(h)]
  * over the request's cache rows 0 .. cache_len[b] - 1 and the rows k_new, v_new of the nodes that i sees.  The cache is
  * only read: sonic_cache_append adds the rows that are kept.
- *   max_ctx         host bound: cache_len[b] <= max_ctx for every b; 0 for empty caches
+ *   max_ctx         host bound, at most 2^30: cache_len[b] <= max_ctx for every b; 0 for empty caches
  *   k_cache, v_cache   device bf16 [rows][Hkv][d] with k_scale = v_scale = NULL, or 4-bit rows with their scales; then the
  *                   nodes' rows are rounded as sonic_cache_append would, and take part at their 4-bit values
  *   q               device bf16 [total_nodes][Hq][d];  k_new, v_new: device bf16 [total_nodes][Hkv][d]
@@ -668,8 +668,8 @@ size_t sonic_tree_decode_workspace_bytes(int32_t batch, int32_t max_nodes, int32
  *                   one for bf16: the output is then off by about 1.3 times its own rounding
  *   workspace       device, 256-byte aligned, >= sonic_tree_decode_workspace_bytes(B, max_nodes, Hq, d, max_ctx) bytes;
  *                   contents need no initialisation.  Calls that share one must not run concurrently
- *   dev_status      SONIC_ERR_CAPACITY when cache_len[b] is negative or above max_ctx: the request's outputs are
- *                   not written, the others' are
+ *   dev_status      SONIC_ERR_CAPACITY when cache_len[b] of a request with nodes is negative or above max_ctx: its
+ *                   outputs are not written, the others' are
  * A value of a node's V that is no number reaches the nodes that see it only.  Reproducible.
  */
 int32_t sonic_tree_decode(int32_t batch, int32_t total_nodes, int32_t max_nodes, int32_t num_q_heads, int32_t num_kv_heads,

@@ -953,7 +953,7 @@ int32_t sonic_tree_decode(int32_t batch, int32_t total_nodes, int32_t max_nodes,
   if (Hq <= 0 || Hkv <= 0 || max_ctx < 0) return SONIC_ERR_INVALID_ARG;
   if (d != 64 && d != 128) return SONIC_ERR_UNSUPPORTED;
   if (Hq % Hkv != 0 || (out_bf16 != 0 && out_bf16 != 1)) return SONIC_ERR_INVALID_ARG;
-  if (Hq / Hkv > 8 || Hkv > 65535) return SONIC_ERR_UNSUPPORTED;
+  if (Hq / Hkv > 8 || Hkv > 65535 || max_ctx > kMaxTreeCtx) return SONIC_ERR_UNSUPPORTED;
   if (!std::isfinite(softmax_scale) || softmax_scale < 0.f) return SONIC_ERR_INVALID_ARG;
   softmax_scale = default_scale(softmax_scale, d);
   const int32_t st = check_plan(batch, total_nodes, max_nodes, plan, plan_bytes, dev_status);
@@ -966,7 +966,7 @@ int32_t sonic_tree_decode(int32_t batch, int32_t total_nodes, int32_t max_nodes,
     return SONIC_ERR_INVALID_ARG;
   const TreeShape sh = tree_shape(batch, Hkv, Hq / Hkv, d, max_nodes, max_ctx, k_scale != nullptr);
   if (workspace_bytes < sh.part_bytes) return SONIC_ERR_WORKSPACE;
-  if ((static_cast<long>(batch) * Hkv * sh.splits + kNumXcd) * sh.tiles > INT32_MAX) return SONIC_ERR_UNSUPPORTED;   // the grid
+  if ((static_cast<long>(batch) * Hkv * sh.splits + kNumXcd) * sh.tiles * 4 * kWave > UINT32_MAX) return SONIC_ERR_UNSUPPORTED;   // a grid's threads
   TreeCall c{};
   c.batch = batch, c.total_nodes = total_nodes, c.max_nodes = max_nodes, c.max_ctx = max_ctx;
   tree_plan_layout(batch, total_nodes, max_nodes, plan, &c.plan);
@@ -1045,7 +1045,7 @@ int32_t sonic_logits_process(int32_t batch, int32_t total_rows, int32_t max_node
     max_nodes = 1;
   }
   if (batch == 0 || total_rows == 0 || max_nodes == 0) return SONIC_OK;
-  if (!logits || !workspace || (!out && !best && !best_value)) return SONIC_ERR_INVALID_ARG;
+  if (!logits || !workspace || out == logits || (!out && !best && !best_value)) return SONIC_ERR_INVALID_ARG;
   if (tokens != nullptr ? !token_off || !token_len : token_off || token_len || prompt_len) return SONIC_ERR_INVALID_ARG;
   if ((bias_token != nullptr) != (bias_cu != nullptr) || (bias_value != nullptr) != (bias_cu != nullptr)) return SONIC_ERR_INVALID_ARG;
   if (!aligned(logits, 16) || !aligned(out, 16) || !aligned(allowed, 4) || !aligned(workspace, 256)) return SONIC_ERR_INVALID_ARG;

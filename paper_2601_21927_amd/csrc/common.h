@@ -279,7 +279,7 @@ struct DecodeShape {
 
 // A plan of drafted tokens: of each request its first node and its nodes, and of each node the nodes that it sees
 // (bit j % 32 of word j / 32: node j of its request), `words` words a node.
-constexpr int kMaxNodes = 256;
+constexpr int kMaxNodes = 256, kMaxTreeCtx = 1 << 30;
 struct TreePlan {
   const int2 *req;
   const uint32_t *sees;
@@ -304,7 +304,7 @@ struct TreeCall {
 // How such a call is cut into workgroups, and its workspace.
 struct TreeShape {
   int columns;        // q rows of a workgroup, in blocks of 16
-  int waves;          // of a workgroup of up to 32 rows
+  int waves;          // of a workgroup
   int tiles;          // of them in the largest request
   int splits;         // ranges of a request of max_ctx rows
   int range;          // 32-row blocks of a range

@@ -138,30 +138,31 @@ __global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int
   int token = -1;
   if (c.node_token != nullptr && c.plan.req != nullptr && static_cast<int>(threadIdx.x) < r.rows) token = c.node_token[r.first + threadIdx.x];
   int t[AHEAD];
-  auto request = [&](int i0) {
+  const unsigned len = r.len, biases = r.biases;   // (unsigned: indexes go past them by up to 2,048)
+  auto request = [&](unsigned i0) {
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const int i = i0 + k * kLogitThreads;
-      t[k] = i < r.len ? c.tokens[r.off + i] : -1;
+      const unsigned i = i0 + k * kLogitThreads;
+      t[k] = i < len ? c.tokens[r.off + i] : -1;
     }
   };
   // the first tokens of the history, the first biases and the first row are on their way together
   request(threadIdx.x);
-  const int bias = static_cast<int>(threadIdx.x) < r.biases ? c.bias_token[r.bias0 + threadIdx.x] : -1;
+  const int bias = threadIdx.x < biases ? c.bias_token[r.bias0 + threadIdx.x] : -1;
   Parts x;
   x.load(c, r.first + row0, t0, t1);
-  for (int i0 = threadIdx.x; i0 < r.len; i0 += AHEAD * kLogitThreads) {
+  for (unsigned i0 = threadIdx.x; i0 < len; i0 += AHEAD * kLogitThreads) {
     if (i0 >= AHEAD * kLogitThreads) request(i0);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k)
       if (in_piece(t[k])) {
-        if (i0 + k * kLogitThreads < r.prompt) atomicOr(&s_word[t[k] - t0], kSeen);
+        if (i0 + k * kLogitThreads < static_cast<unsigned>(r.prompt)) atomicOr(&s_word[t[k] - t0], kSeen);
         else atomicAdd(&s_word[t[k] - t0], 1u);
         has(t[k] - t0);
       }
   }
-  if (r.biases > 0) {
-    for (int i = threadIdx.x; i < r.biases; i += kLogitThreads) {   // (few tokens of the piece have one: theirs start at -1)
+  if (biases > 0) {
+    for (unsigned i = threadIdx.x; i < biases; i += kLogitThreads) {   // (few tokens of the piece have one: theirs start at -1)
       const int t = i < kLogitThreads ? bias : c.bias_token[r.bias0 + i];
       if (in_piece(t)) {
         atomicOr(&s_word[t - t0], kBiased);
@@ -170,9 +171,9 @@ __global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int
       }
     }
     lds_barrier();
-    for (int i = threadIdx.x; i < r.biases; i += kLogitThreads) {
+    for (unsigned i = threadIdx.x; i < biases; i += kLogitThreads) {
       const int t = i < kLogitThreads ? bias : c.bias_token[r.bias0 + i];
-      if (in_piece(t)) atomicMax(&s_entry[t - t0], i);              // of several entries for a token the last one counts
+      if (in_piece(t)) atomicMax(&s_entry[t - t0], static_cast<int>(i));              // of several entries for a token the last one counts
     }
   }
   const float rep = c.repetition != nullptr ? c.repetition[b] : 1.f;

@@ -4,17 +4,22 @@
 // and over the nodes on i's path (itself and its ancestors),
 //     out[i][h] = softmax_r(scale <q[i][h], k[r][g(h)]>) v[r][g(h)].
 //
-// tree_kernel: a workgroup has up to 64 q rows (node i and q-head g of a kv-head are row i G + g) and a range of the
-// request's rows, in blocks of 32: first the cache's, then the nodes', so that a block is of one kind and the nodes'
-// visibility in it is one word of the plan.  The four waves take blocks in turn, each with its own K and V in LDS
-// (direct-to-LDS loads, K of the next block requested when this one's scores are taken, V when its values are), so that
-// none waits for another before the end.  Per block
+// A workgroup has a tile of q rows (node i and q-head g of a kv-head are row i G + g) and a range of the request's rows, in
+// blocks of 32: first the cache's, then the nodes', so that a block is of one kind and the nodes' visibility in it is one
+// word of the plan.  Per block and wave
 //   scores   S^T (16 rows x 16 columns) = K . Q^T   v_mfma_f32_16x16x32_bf16
 //   softmax  online, fp32, per column in the four lanes that hold it
 //   values   O^T (d x 16 columns) += V^T . P^T      v_mfma_f32_16x16x32_bf16, depth 32: the block's rows
+// K and V come by direct-to-LDS loads.  Up to 32 rows are one wave's columns, and the waves of a workgroup take blocks in
+// turn, each with LDS of its own (tree_kernel); of more rows, waves with 32 each share the blocks (tree_wide_kernel).
 // An fp32 output takes a probability in three bf16 values (2^-26 of it is left), a bf16 output in one: its rounding, with
 // the sum taken over the rounded ones, is of the size of the output's own (1.2 to 1.3 times that in all).
 // Ranges of a request are joined by another kernel.
+//
+// Bound by, trees of 32 over eight caches of 1,328 rows (32 / 8 heads of 128, bf16 out, 17.7 us; the bytes alone 9.5, the
+// products 4.6): 2.2 us until the first rows are asked for, eleven blocks a wave with one wave a SIMD, 2 us for the waves'
+// join.  Long and wide ones by the sum of what the SIMDs issue (chains of 250 over four caches of 1,584, 43 us: matrix cores 14,
+// vector instructions 16, LDS 17; they overlap little, two waves a SIMD).  64 caches of 1,500 rows, trees of 16: HBM, 5.1 TB/s.
 #include <algorithm>
 
 #include "common.h"
@@ -27,7 +32,6 @@ typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16_t;
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTreeWaves = 4;
 constexpr int kTreeBlock = 32;   // rows of a block: the bits of a word of the plan
 
 // ------------------------------------------------------------------ the plan
@@ -216,7 +220,7 @@ template <int D, int CT, int PARTS> struct TreeColumns {
   f32x4 oacc[CT][DB];                            // lane (col, quarter): d = 16 db + 4 quarter .. + 3 of column 16 t + col
   float m_run[CT];                               // log2 domain, lagging by at most 8
   f32x4 lacc[CT];                                // the probabilities' sum, in every element: a product with ones, of the same
-                                                 // rounded values as the output's
+                                                 // rounded values as the output's (4 % faster than adding them up)
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -348,7 +352,7 @@ __device__ __forceinline__ void tree_mask(const TreeCall &c, const TreeReq &r, i
   }
 }
 
-// V of a block of nodes in LDS: what is no number becomes zero (see tree_store).  Returns whether there was any.
+// V of a block of nodes in LDS: what is no number becomes zero (see tree_odd_values).  Returns whether there was any.
 template <int D> __device__ __forceinline__ bool tree_only_numbers(uint16_t *vtile, int lane) {
   bool here = false;
 #pragma unroll
@@ -1016,7 +1020,7 @@ TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ct
 
 template <int D, bool Q4, int PARTS>
 static void launch_tree_rows(const TreeCall &c, const TreeShape &sh, float *part, int Hkv, int G, dim3 grid, hipStream_t stream) {
-  const dim3 block(kTreeWaves * kWave), more(8 * kWave);
+  const dim3 block(4 * kWave), more(8 * kWave);
   if (sh.columns == 1 && sh.waves == 8) tree_kernel<D, 1, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, part, Hkv, G);
   else if (sh.columns == 1) tree_kernel<D, 1, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
   else if (sh.columns == 2 && sh.waves == 8) tree_kernel<D, 2, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, part, Hkv, G);
@@ -1096,7 +1100,7 @@ __global__ __launch_bounds__(kWave) void tree_accept_kernel(TreePlan plan, const
   if (tokens != nullptr) {
     const int len = token_len[b], cap = token_cap[b];
     const int64_t off = token_off[b];
-    if (len < 0 || steps > cap - len) {   // no room: nothing of the request is kept
+    if (len < 0 || cap < len || steps > cap - len) {   // no room: nothing of the request is kept
       if (lane == 0) raise_status(status, SONIC_ERR_CAPACITY);
       steps = 0, want = -1;
 #pragma unroll

@@ -558,6 +558,8 @@ def logits_process(logits, best, workspace, dev_status, plan=None, batch=None, m
     node_token int32 [n]; tokens int32 with token_off int64 [B], token_len and prompt_len int32 [B]; repetition, presence,
     frequency fp32 [B]; bias_cu int32 [B+1], bias_token int32 and bias_value fp32; allowed int32 [n,(V+31)//32]."""
     n, V = logits.shape
+    if plan is not None and batch is None:
+        raise ValueError("a plan comes with the batch that it was made for")
     B = int(batch) if batch is not None else n
     if logits.dtype not in (_F32, _BF16):
         raise TypeError(f"logits must be {_F32} or {_BF16}, got {logits.dtype}")

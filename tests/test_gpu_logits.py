@@ -218,3 +218,43 @@ def test_two_streams_and_graphs():
             c.parts, c.allowed = {"path", "penalties"}, None
             c.pres, c.freq = np.zeros(c.B), np.zeros(c.B)
             c.check()
+
+
+def test_elements_past_32_bits():
+    """17,000 rows of 130,001 bf16 logits, 2.2e9 of them: the last rows as a call of their own does them."""
+    H.need_gpu()
+    n, V = 17000, 130001
+    gen = torch.Generator(device="cuda").manual_seed(16)
+    some = torch.randn((40, V), device="cuda", generator=gen).to(torch.bfloat16)
+    x = torch.zeros((n, V), dtype=torch.bfloat16, device="cuda")
+    x[:20], x[-20:] = some[:20], some[20:]
+    best, value = [torch.zeros(m, dtype=torch.int32, device="cuda") for m in (n, 40)], [torch.zeros(m, device="cuda") for m in (n, 40)]
+    token = torch.zeros(n, dtype=torch.int32, device="cuda")
+    token[-20:] = some[20:].argmax(1).int()
+    rep, status = torch.full((n,), 3.0, device="cuda"), i32([0])
+    out = torch.zeros((40, V), device="cuda")
+    for i, (rows, t, o) in enumerate(((x, token, None), (some, torch.cat([token[:20], token[-20:]]), out))):
+        ws = torch.empty(sonic.logits_process_workspace_bytes(len(t), V), dtype=torch.uint8, device="cuda")
+        assert sonic.logits_process(rows, best[i], ws, status, node_token=t, repetition=rep[:len(t)], best_value=value[i], out=o) == sonic.OK
+    torch.cuda.synchronize()
+    assert torch.equal(torch.cat([best[0][:20], best[0][-20:]]), best[1]) and torch.equal(torch.cat([value[0][:20], value[0][-20:]]), value[1])
+    want = some.float().cpu().numpy()          # (on the host: a division of a GPU tensor by a number is a product with its inverse)
+    at = (np.arange(40), np.concatenate([token[:20].cpu().numpy(), token[-20:].cpu().numpy()]))
+    want[at] = np.where(want[at] > 0, want[at] / np.float32(3), want[at] * np.float32(3))
+    assert np.array_equal(out.cpu().numpy(), want) and np.array_equal(value[1].cpu().numpy(), want.max(1))
+
+
+def test_many_biases_and_histories_without_a_prompt():
+    """More biases than a workgroup has threads, a token several times among them; all of a history generated."""
+    H.need_gpu()
+    for nodes in (None, [3, 1]):
+        c = Call(np.random.default_rng(17), 2, 700, nodes=nodes, hist=3000, biases=0)
+        rng = np.random.default_rng(18)
+        c.bias_cu = np.array([0, 1400, 2011], np.int32)
+        c.bias_token = rng.integers(0, 700, 2011).astype(np.int32)
+        c.bias_value = rng.standard_normal(2011).astype(np.float32)
+        c.parts.add("biases")
+        c.prompt[:] = 0
+        c.run().check()
+        c.prompt[:] = c.len
+        c.run(out=False).check()

@@ -386,3 +386,53 @@ def test_rows_past_4_gib():
             p = np.exp(s - top)
             want = (p @ vv) / (p.sum() + last * np.exp(-top))
             assert np.abs(out[4 + i, h].double().cpu().numpy() - want).max() <= bar * np.abs(vv).max()
+
+
+# ------------------------------------------------------------------ how a call is cut
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+@pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B", [17, 33])
+def test_every_cut(B, d, q4, out):
+    """Tiles of 16 to 128 rows in four and eight waves: 136 and 264 (request, kv-head) pairs, up to 16, 32, 64, 128 and 136 rows a
+    kv-head, one long context among short ones; each with all values numbers, and with some that are none."""
+    H.need_gpu()
+    rng = np.random.default_rng(B + d + q4)
+    lens = rng.integers(0, 60, B)
+    lens[3] = 3300
+    c = Cache(rng, lens, 1, 8, d, q4)
+    for most in (8, 16, 32, 64, 68):
+        nodes = [int(x) for x in rng.integers(0, 4, B)]
+        nodes[3], nodes[5] = most // 2 + 1, most
+        s = Step(rng, c, 16, nodes)
+        s.check(s.run(out), out)
+        s.v[int(s.cu[5]) + 2, 4, 9] = 0x7FC0                       # one node's value: NaN
+        got = s.run(out)
+        for b in (3, 5):
+            want, top = s.expect(b)
+            mine = got[s.cu[b]:s.cu[b + 1]]
+            assert np.array_equal(np.isnan(mine), np.isnan(want)), b
+            fine = ~np.isnan(want)
+            assert np.all(np.abs(mine[fine] - want[fine]) <= BAR[out] * top)
+
+
+def test_two_calls_at_once():
+    """Side by side on two streams, each with its own workspace and the same cache and plan."""
+    H.need_gpu()
+    rng = np.random.default_rng(41)
+    c = Cache(rng, [6000, 300], 1, 2, 128, False)
+    steps = [Step(rng, c, 8, [9, 3]) for _ in range(2)]
+    steps[1].parents, steps[1].parent = steps[0].parents, steps[0].parent
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    assert steps[0].step.plan_trees(i32(steps[0].cu), steps[0].parent, c.status) == sonic.OK
+    dev = [[bf16_to_device(x) for x in (s.q, s.k, s.v)] for s in steps]
+    out = [torch.zeros((12, 8, 128), device="cuda") for _ in steps]
+    ws = [torch.empty(sonic.tree_decode_workspace_bytes(2, 9, 8, 128, 6000), dtype=torch.uint8, device="cuda") for _ in steps]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, stream in enumerate(streams):
+            assert sonic.tree_decode(steps[0].step.plan, c.dev.k, c.dev.v, c.dev.row_off, c.dev.length, *dev[i], out[i], ws[i], c.status, 9, 6000,
+                                     stream=stream) == sonic.OK
+    torch.cuda.synchronize()
+    for s, o in zip(steps, out):
+        s.check(o.double().cpu().numpy())

@@ -83,9 +83,10 @@ def test_full_histories_and_pending_errors():
     a = Accept(np.random.default_rng(2), [6, 9, 4, 5], "chain", tokens=1)
     a.hist_cap[1] = a.hist_len[1] + 8          # one place short
     a.hist_len[2] = -1
-    a.run().check(full=(1, 2))
+    a.hist_cap[3] = -2 ** 31
+    a.run().check(full=(1, 2, 3))
     assert int(a.status.item()) == sonic.ERR_CAPACITY
-    a.run().check(full=(1, 2))                 # pending: stops nothing
+    a.run().check(full=(1, 2, 3))              # pending: stops nothing
     before = a.step.path.clone()
     a.status.fill_(sonic.ERR_BAD_LAYOUT)
     a.chosen[:] = -1
@@ -172,6 +173,7 @@ def test_append_errors_leave_the_request_and_do_the_others(q4):
     at = lambda a, i, x: np.concatenate([a[:i], [x], a[i + 1:]])  # noqa: E731
     case(sonic.ERR_CAPACITY, cap=12)
     case(sonic.ERR_CAPACITY, cap=-5)
+    case(sonic.ERR_CAPACITY, cap=-2 ** 31)
     case(sonic.ERR_BAD_LAYOUT, length=-1)
     case(sonic.ERR_BAD_LAYOUT, select=at(full, 22, 3))
     case(sonic.ERR_BAD_LAYOUT, select=at(full, 23, -1))
@@ -347,3 +349,75 @@ def test_steps_generate_what_token_by_token_decode_does(q4):
         for c, o in zip(caches, one):
             rows = slice(int(c.row_off_host[b]), int(c.row_off_host[b]) + m)
             assert torch.equal(c.k[rows], o.k[rows]) and torch.equal(c.v[rows], o.v[rows])
+
+
+def test_a_captured_step_replayed():
+    """Plan, two layers, logits, accept and append as one graph, replayed step after step with the program's own work between:
+    the caches, histories and tokens are those of the same calls made one by one."""
+    H.need_gpu()
+    B, Hq, Hkv, d, V, n = 2, 4, 2, 64, 50, 12
+    runs = []
+    for captured in (False, True):
+        rng = np.random.default_rng(31)
+        model = Model(rng, Hq, Hkv, d, V)
+        caches = make_caches(rng, [60, 300], 40, Hkv, d, False)
+        for c in caches:
+            for x in (c.k, c.v):
+                x.copy_(bf16_to_device(normal_bits(rng, x.shape[0], Hkv, d)))
+            c.length.copy_(i32([60, 300]))
+        status, step = i32([0]), DraftStep(B, n, 8)
+        cu, parent, token, chosen = i32([0, 0, 0]), i32([0] * n), i32([0] * n), i32([0] * n)
+        tokens, off, lens = i32(rng.integers(0, V, 200)), torch.tensor([0, 100], device="cuda"), i32([20, 30])
+        out = [torch.zeros((n, Hq, d), device="cuda") for _ in caches]
+        logits = torch.zeros((n, V), device="cuda")
+
+        def attention():
+            assert step.plan_trees(cu, parent, status) == sonic.OK
+            for i, c in enumerate(caches):
+                assert c.tree_decode(step.plan, q[i], k[i], v[i], out[i], status, 8, 340) == sonic.OK
+
+        def rest():
+            assert step.logits(logits, status, node_token=token, tokens=tokens, token_off=off, token_len=lens,
+                               frequency=frequency) == sonic.OK
+            assert step.accept(parent, token, status, chosen=chosen, tokens=tokens, token_off=off, token_cap=cap, token_len=lens) == sonic.OK
+            for i, c in enumerate(caches):
+                assert c.append(cu, k[i], v[i], status, 8, select=step.path, select_len=step.path_len) == sonic.OK
+        frequency, cap = torch.full((B,), 0.5, device="cuda"), i32([100] * B)
+        q, k, v = ([torch.zeros((n, h, d), dtype=torch.bfloat16, device="cuda") for _ in caches] for h in (Hq, Hkv, Hkv))
+        parts = [attention, rest]
+        if captured:
+            attention()                                    # (no nodes yet: nothing changes)
+            rest()
+            torch.cuda.synchronize()
+            graphs = []
+            for part in parts:
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g):
+                    part()
+                graphs.append(g.replay)
+            parts = graphs
+        seen = []
+        for turn in range(4):
+            nodes = [int(x) for x in rng.integers(1, 6, B)]
+            m = sum(nodes)
+            flat = np.concatenate([tree(rng, x) for x in nodes])
+            cu.copy_(i32(np.concatenate([[0], np.cumsum(nodes)])))
+            parent[:m] = i32(flat)
+            token[:m] = i32(rng.integers(0, 3, m))
+            for i in range(2):
+                for x, table in ((q, model.q), (k, model.k), (v, model.v)):
+                    x[i].copy_(table[i][token.long()])
+            parts[0]()
+            logits.copy_(model.logits(out))
+            chosen[:m] = i32(rng.integers(0, 3, m))
+            parts[1]()
+            torch.cuda.synchronize()
+            assert int(status.item()) == 0
+            seen += [x.clone() for x in (step.path[:m], step.path_len, step.next_token, step.best[:m], lens, tokens, *[c.length for c in caches])]
+        for c in caches:
+            for b in range(B):
+                rows = slice(int(c.row_off_host[b]), int(c.row_off_host[b]) + int(c.length[b]))
+                seen += [c.k[rows].clone(), c.v[rows].clone()]
+        runs.append(seen)
+    assert len(runs[0]) == len(runs[1]) and all(torch.equal(a, b) for a, b in zip(*runs))
+    assert runs[0][-1].shape[0] >= 304                     # every step adds its tree's first node at least

@@ -89,6 +89,8 @@ def test_decode_arguments():
     assert decode(Hq=5) == sonic.ERR_INVALID_ARG
     assert decode(Hq=18) == sonic.ERR_UNSUPPORTED             # nine q-heads a kv-head
     assert decode(ctx=-1) == sonic.ERR_INVALID_ARG
+    assert decode(ctx=(1 << 30) + 1) == sonic.ERR_UNSUPPORTED and decode(ctx=1 << 30) == sonic.OK
+    assert decode(B=65535, Hq=65535, Hkv=65535, N=1 << 30) == sonic.ERR_UNSUPPORTED     # more workgroups than a launch has
     assert decode(ctx=0) == sonic.OK
     assert decode(bf16=2) == sonic.ERR_INVALID_ARG
     for scale in (-1.0, float("nan"), float("inf")):
@@ -112,7 +114,7 @@ def test_alignment(fn, names):
         assert fn(**ONE[fn], **{n: ODD}) == sonic.ERR_INVALID_ARG, n
 
 
-@pytest.mark.parametrize("B,nodes,Hq,Hkv,d,ctx", [(1, 8, 4, 2, 64, 700), (8, 32, 32, 8, 128, 1328), (1, 256, 32, 8, 128, 100001), (1, 1, 1, 1, 64, 9000)])
+@pytest.mark.parametrize("B,nodes,Hq,Hkv,d,ctx", [(1, 8, 4, 2, 64, 2000), (8, 8, 32, 8, 128, 5000), (1, 64, 32, 8, 128, 100001), (1, 1, 1, 1, 64, 9000)])
 def test_small_workspaces(B, nodes, Hq, Hkv, d, ctx):
     need = sonic.tree_decode_workspace_bytes(B, nodes, Hq, d, ctx)
     shape = dict(B=B, N=B * nodes, nodes=nodes, Hq=Hq, Hkv=Hkv, d=d, ctx=ctx)
@@ -143,6 +145,7 @@ def test_logits_arguments():
     assert logits(bf16=2) == sonic.ERR_INVALID_ARG
     one = dict(B=1, N=1)
     assert logits(**one, best=None) == sonic.ERR_INVALID_ARG   # nothing to write
+    assert logits(**one, out=P) == sonic.ERR_INVALID_ARG       # over the logits themselves
     for n in ("hoff", "hlen", "plen", "hist"):
         assert logits(**one, **{n: P}) == sonic.ERR_INVALID_ARG
     assert logits(**one, hist=P, hoff=P) == sonic.ERR_INVALID_ARG
@@ -165,6 +168,8 @@ def test_binding_refuses_host_tensors_wrong_types_and_shapes():
         sonic.logits_process(torch.zeros((2, 8), dtype=torch.float16), i, u, i)
     with pytest.raises(ValueError):
         sonic.logits_process(torch.zeros((2, 8)), i, u, i)
+    with pytest.raises(ValueError):
+        sonic.logits_process(torch.zeros((2, 8)), i[:2], u, i, plan=u)      # without its batch
     with pytest.raises(ValueError):
         sonic.tree_accept(u, None, i, i, i, i, i, i, 4)
     with pytest.raises(ValueError):
