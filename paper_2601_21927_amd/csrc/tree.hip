@@ -735,11 +735,10 @@ again:
 }
 
 // More than 32 q rows: RW waves with 32 of them each share the blocks in LDS, KW = NW / RW such groups take the NW / 2 blocks of
-// a step between them.  While a step is computed the next rows stream into the other buffers: K of step c + 2 once
-// every wave has taken its scores of step c, V of step c + 1 once every wave is done with that of c - 1.  Each wave issues
-// NJ direct-to-LDS loads per tensor and step, in the order K(0) V(0) K(1) | V(1) K(2) | .., also past the end (there the last
-// block again), so at either wait all but the 2 NJ most recent are what is waited for.  4-bit rows are decoded on the way:
-// the codes of a step ahead wait in registers, one quantisation block a lane.
+// a step between them.  While a step is computed the next one's rows stream into the other buffers, NJ direct-to-LDS loads a
+// wave and tensor, also past the end (there the last block again).  One barrier a step, before its rows are read: a second one
+// behind the scores, with K a step further ahead, left the waves less room (64 requests of 180 .. 4,300 rows: 115 us, this
+// way 109).  4-bit rows are decoded on the way: the codes of a step ahead wait in registers, one quantisation block a lane.
 template <int D, int RW, int NW, bool Q4, int PARTS>
 __global__ __launch_bounds__(NW *kWave, 2) void tree_wide_kernel(TreeCall c, TreeShape sh, float *__restrict__ part, int Hkv, int G) {
   typedef TreeColumns<D, 2, PARTS> Columns;
@@ -774,18 +773,14 @@ __global__ __launch_bounds__(NW *kWave, 2) void tree_wide_kernel(TreeCall c, Tre
   const int full = r.len / BR;                       // blocks without a row that some column does not see
   bool careful = false, odd = false;
 
-  // One step: `between` runs behind the scores (the V of the step is there when it returns).
-  auto compute = [&](int step, auto between) {
+  auto compute = [&](int step) {
+    if (rowless) return;
     const uint16_t *kt = kbuf + (step & 1) * SB * TILE;
     uint16_t *vt = vbuf + (step & 1) * SB * TILE;
     f32x4 s[NB][CT][2];
-    if (!rowless) {
 #pragma unroll
-      for (int n = 0; n < NB; ++n) cols.scores(kt + (KW * n + kg) * TILE, qf, col, quarter, s[n]);
-      order_operands<NB * 2 * KS, 1, CT, kAheadK>();
-    }
-    between();
-    if (rowless) return;
+    for (int n = 0; n < NB; ++n) cols.scores(kt + (KW * n + kg) * TILE, qf, col, quarter, s[n]);
+    order_operands<NB * 2 * KS, 1, CT, kAheadK>();
     const int g = first + SB * step + kg;
     if (__builtin_expect(g + KW * (NB - 1) >= full, 0))
 #pragma unroll
@@ -825,17 +820,13 @@ again:
     auto issue_v = [&](int step) { issue(step, vbase, vnew, at + 4 * SB * TILE, true); };
     issue_k(0);
     issue_v(0);
-    issue_k(1);
     tree_wait(qf);
     for (int step = 0; step < steps; ++step) {
-      wait_vm<2 * NJ>();
-      lds_barrier();   // K of the step is there; every wave is past the values of the one before
+      wait_vm<0>();
+      lds_barrier();   // the step's rows are there; every wave is past the one before
+      issue_k(step + 1);
       issue_v(step + 1);
-      compute(step, [&]() {
-        wait_vm<2 * NJ>();
-        lds_barrier();   // V of the step is there; every wave has its scores
-        issue_k(step + 2);
-      });
+      compute(step);
     }
     wait_vm<0>();
   } else {
@@ -896,7 +887,7 @@ again:
       lds_barrier();   // the step's rows are there; every wave is past the one before
       put(step + 1);
       fetch_both(step + 2);
-      compute(step, []() {});
+      compute(step);
     }
   }
 
@@ -994,8 +985,8 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeCall c, Tre
 //   4-bit rows are decoded once for each tile.
 // - Ranges: up to 256 workgroups, of 512 rows and more (1,024 from 128 tiles on: the join is a launch of 4 us).  One request
 //   of 8,000 rows, trees of 16: 4 ranges 20.8 us, 8 16.1, 16 18.0; 8 of 1,328 rows, trees of 8: one range 14.7, two 16.1.
-//   Uneven lengths are not evened out: 64 requests of 180 .. 4,300 rows, trees of up to 16, took 114 us in one range each, 106 to
-//   109 in three or in ranges shared evenly over the batch, which cost 64 equal ones of 1,500 rows 85 us instead of 77.
+//   Uneven lengths are not evened out: 64 requests of 180 .. 4,300 rows, trees of up to 16, gained 5 to 8 us of 114 in three
+//   ranges or in ranges shared evenly over the batch, which cost 64 equal ones of 1,500 rows 85 us instead of 77.
 // - Eight waves where a CU has one workgroup: of up to 32 rows if it is long (4 requests of 7,552 rows, 28 / 4 heads, trees of
 //   61, fp32: 67 us, with four 73; one of 100,001 4-bit rows: 16 ranges of eight waves 73, 32 of four 74, and 16 of four 99),
 //   of more rows always (chains of 250 over four requests of 1,584 rows 42.6 and 49.9; trees of 64 over eight of 1,328 24.5
