@@ -12,8 +12,10 @@
 // in which a thread's tokens that have a word are mended one after the other: there are few, but most waves have some
 // among any 256 tokens, and did the penalties' divisions for all of them (256 rows of 128,000 in bf16, written out: 73 us
 // so, 62 this way).  The next row's logits, mask words and path are requested ahead of this row's stores, so that a row
-// waits for nothing of its own (55 us; 201 MB, 3.7 TB/s).  Where rows are few, a chain of loads is what counts: lengths, then
-// history and logits, then biases (64 rows of 150,001 with histories of up to 9,000 tokens, 41 MB: 26 us).
+// waits for nothing of its own (55 us), and the stores pass the caches, which hold what the program has just computed (45 us;
+// 201 MB, 4.5 TB/s).  Where rows are few, a chain of loads is what counts: lengths, then history and logits, then biases, in
+// 2.3 rounds of workgroups, and the vector instructions of the histories' scan, which every piece makes again (64 rows of
+// 150,001 with histories of up to 9,000 tokens, 41 MB: 25 us, half of them issuing).
 // logits_best_kernel picks each row's best from the pieces' and raises errors.
 #include <algorithm>
 
@@ -244,7 +246,8 @@ __global__ __launch_bounds__(kLogitThreads) void logits_kernel(LogitsCall c, int
         float *o = c.out + start + t;
         if (t >= t0 && t + PE <= t1) {
 #pragma unroll
-          for (int e = 0; e < PE; e += 4) *reinterpret_cast<f32x4 *>(o + e) = f32x4{v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3]};
+          for (int e = 0; e < PE; e += 4)
+            __builtin_nontemporal_store(f32x4{v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3]}, reinterpret_cast<f32x4 *>(o + e));
         } else {
 #pragma unroll
           for (int e = 0; e < PE; ++e)
