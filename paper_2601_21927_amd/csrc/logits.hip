@@ -14,8 +14,8 @@
 // so, 62 this way).  The next row's logits, mask words and path are requested ahead of this row's stores, so that a row
 // waits for nothing of its own (55 us), and the stores pass the caches, which hold what the program has just computed (45 us;
 // 201 MB, 4.5 TB/s).  Where rows are few, a chain of loads is what counts: lengths, then history and logits, then biases, in
-// 2.3 rounds of workgroups, and the vector instructions of the histories' scan, which every piece makes again (64 rows of
-// 150,001 with histories of up to 9,000 tokens, 41 MB: 25 us, half of them issuing).
+// 2.3 rounds of workgroups, and then the histories, which every piece scans again (64 rows of 150,001 with histories of up to
+// 9,000 tokens, 41 MB: 25 us, 7 of them the histories').
 // logits_best_kernel picks each row's best from the pieces' and raises errors.
 #include <algorithm>
 

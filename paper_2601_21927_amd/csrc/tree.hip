@@ -18,8 +18,9 @@
 //
 // Bound by, trees of 32 over eight caches of 1,328 rows (32 / 8 heads of 128, bf16 out, 17.7 us; the bytes alone 9.5, the
 // products 4.6): 2.2 us until the first rows are asked for, eleven blocks a wave with one wave a SIMD, 2 us for the waves'
-// join.  Long and wide ones by the sum of what the SIMDs issue (chains of 250 over four caches of 1,584, 43 us: matrix cores 14,
-// vector instructions 16, LDS 17; they overlap little, two waves a SIMD).  64 caches of 1,500 rows, trees of 16: HBM, 5.1 TB/s.
+// join.  Long and wide ones by the sum of what the SIMDs do (chains of 250 over four caches of 1,584, 43 us: matrix cores 14,
+// vector instructions 14, LDS 7 and waits for it; they overlap little, two waves a SIMD).  64 caches of 1,500 rows, trees of
+// 16: HBM, 5.1 TB/s.
 #include <algorithm>
 
 #include "common.h"
@@ -901,7 +902,8 @@ again:
 
 // The ranges of a request joined by log-sum-exp.  Grid (rows of a kv-head / rows a workgroup has, kv-heads, requests).  A
 // thread has four values of a row and every sh.groups-th range of it; the groups' parts meet in LDS.  The first ranges are
-// loaded before the request is looked up: their places do not depend on it.
+// loaded before the request is looked up: their places do not depend on it.  16 ranges of 52 rows a kv-head: 4.2 us, a launch
+// and two round trips.
 constexpr int kJoinThreads = 256, kJoinAhead = 4;
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeCall c, TreeShape sh, const float *__restrict__ part, int G) {
@@ -1048,7 +1050,8 @@ hipError_t launch_tree(const TreeCall &c, const TreeShape &sh, float *part, int 
 
 // ------------------------------------------------------------------ the path that is kept
 // One wave per request.  From node 0 on: of the nodes behind the present one whose parent it is and whose token is the one
-// chosen there, the lowest; until there is none.  Lane l looks at nodes l, l + 64, ..: a step is a few ballots.
+// chosen there, the lowest; until there is none.  Lane l looks at nodes l, l + 64, ..: a step is a few ballots.  Bound by the
+// round trips before them and the stores behind: 4.3 us for eight trees of 32.
 __global__ __launch_bounds__(kWave) void tree_accept_kernel(TreePlan plan, const int32_t *__restrict__ parent, const int32_t *__restrict__ node_token,
                                                             const int32_t *__restrict__ chosen, int32_t *__restrict__ path,
                                                             int32_t *__restrict__ path_len, int32_t *__restrict__ next_token,
