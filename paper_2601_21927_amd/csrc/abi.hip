@@ -966,7 +966,7 @@ int32_t sonic_tree_decode(int32_t batch, int32_t total_nodes, int32_t max_nodes,
     return SONIC_ERR_INVALID_ARG;
   const TreeShape sh = tree_shape(batch, Hkv, Hq / Hkv, d, max_nodes, max_ctx, k_scale != nullptr);
   if (workspace_bytes < sh.part_bytes) return SONIC_ERR_WORKSPACE;
-  if ((static_cast<long>(batch) * Hkv * sh.splits + kNumXcd) * sh.tiles * 4 * kWave > UINT32_MAX) return SONIC_ERR_UNSUPPORTED;   // a grid's threads
+  if ((static_cast<long>(batch) * Hkv * sh.splits + (kNumXcd << sh.run_log2)) * sh.tiles * 4 * kWave > UINT32_MAX) return SONIC_ERR_UNSUPPORTED;   // a grid's threads
   TreeCall c{};
   c.batch = batch, c.total_nodes = total_nodes, c.max_nodes = max_nodes, c.max_ctx = max_ctx;
   tree_plan_layout(batch, total_nodes, max_nodes, plan, &c.plan);

@@ -308,6 +308,7 @@ struct TreeShape {
   int tiles;          // of them in the largest request
   int splits;         // ranges of a request of max_ctx rows
   int range;          // 32-row blocks of a range
+  int run_log2;       // that many kv-heads of a range (2^) are neighbours on one XCD
   int groups;         // threads that share a row's ranges when they are joined
   size_t part_bytes;  // partials: [request][kv-head][tile][split] of the values, then of (max, sum)
 };

@@ -470,13 +470,13 @@ struct TreePlace {
   float *acc;        // the range's partial: the values, ..
   float2 *stat;      // .. and (max, sum), of COLS columns
 };
-// False: nothing to do.  The row tiles of one range are neighbours on one XCD (workgroup i goes to XCD i % 8), as are a
-// range's kv-heads in time: the rows come from its L2 after the first.
+// False: nothing to do.  The row tiles of one range are neighbours on one XCD (workgroup i goes to XCD i % 8): its rows come
+// from that L2 after the first.  So are 2^run_log2 of its kv-heads.
 template <int D, int COLS>
 __device__ __forceinline__ bool tree_begin(const TreeCall &c, const TreeShape &sh, float *part, int Hkv, int G, TreePlace *p) {
   __shared__ int s_stop;
   const unsigned turn = blockIdx.x / kNumXcd, xcd = blockIdx.x % kNumXcd;
-  const unsigned unit = turn / sh.tiles * kNumXcd + xcd;
+  const unsigned at = turn / sh.tiles, unit = ((((at >> sh.run_log2) * kNumXcd + xcd) << sh.run_log2) + (at & ((1u << sh.run_log2) - 1)));
   if (unit >= static_cast<unsigned>(c.batch) * Hkv * sh.splits) return false;
   p->rt = turn % sh.tiles;
   p->kvh = unit % Hkv;
@@ -993,6 +993,9 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeCall c, Tre
 //   61, fp32: 67 us, with four 73; one of 100,001 4-bit rows: 16 ranges of eight waves 73, 32 of four 74, and 16 of four 99),
 //   of more rows always (chains of 250 over four requests of 1,584 rows 42.6 and 49.9; trees of 64 over eight of 1,328 24.5
 //   and 27.6).  With two workgroups a CU four are better (64 requests of 1,500 rows, trees of 16: 78, with eight 84).
+// - Neighbours: lines of 4-bit rows hold several heads' codes and scales, so up to eight heads of a range go to one XCD, as
+//   long as every XCD still gets as many workgroups (64 requests of 1,500 rows, trees of 8: 39.0 us, each head on another XCD
+//   46.5; one of 100,001 rows: 114 MB fetched instead of 266, 70.6 us instead of 72).
 TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ctx, bool q4) {
   TreeShape sh{};
   const long rows = static_cast<long>(max_nodes) * G, pairs = static_cast<long>(batch) * Hkv;
@@ -1006,6 +1009,10 @@ TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ct
   sh.range = static_cast<int>((blocks + splits - 1) / splits + 3) / 4 * 4;   // whole steps
   sh.splits = static_cast<int>((blocks + sh.range - 1) / sh.range);
   sh.waves = units * sh.splits <= 256 && (sh.columns > 2 || sh.range > (q4 ? 32 : 96)) ? 8 : 4;
+  for (sh.run_log2 = 0; q4 && sh.run_log2 < 3 && Hkv % (2 << sh.run_log2) == 0; ++sh.run_log2) {
+    const long unit_groups = pairs * sh.splits >> (sh.run_log2 + 1);
+    if (unit_groups % kNumXcd != 0 && unit_groups < 8 * kNumXcd) break;
+  }
   for (sh.groups = 1; sh.groups < 8 && sh.groups * kJoinAhead < sh.splits; sh.groups *= 2) {}
   sh.part_bytes = sh.splits > 1 ? static_cast<size_t>(units) * sh.splits * 16 * sh.columns * (D + 2) * sizeof(float) : 0;
   return sh;
@@ -1027,7 +1034,8 @@ static void launch_tree_rows(const TreeCall &c, const TreeShape &sh, float *part
 template <int D>
 static void launch_tree_d(const TreeCall &c, const TreeShape &sh, float *part, int Hkv, int G, hipStream_t stream) {
   const long units = static_cast<long>(c.batch) * Hkv * sh.splits;
-  const dim3 grid((units + kNumXcd - 1) / kNumXcd * kNumXcd * sh.tiles);
+  const long each_xcd = static_cast<long>(kNumXcd) << sh.run_log2;
+  const dim3 grid((units + each_xcd - 1) / each_xcd * each_xcd * sh.tiles);
   if (c.ks != nullptr) {
     if (c.out_bf16) launch_tree_rows<D, true, 1>(c, sh, part, Hkv, G, grid, stream);
     else launch_tree_rows<D, true, 3>(c, sh, part, Hkv, G, grid, stream);
