@@ -563,6 +563,10 @@ def logits_process(logits, best, workspace, dev_status, plan=None, batch=None, m
     B = int(batch) if batch is not None else n
     if logits.dtype not in (_F32, _BF16):
         raise TypeError(f"logits must be {_F32} or {_BF16}, got {logits.dtype}")
+    if tokens is not None and tokens.numel() == 0:           # (an empty tensor has no address: no history, ..
+        tokens = token_off = token_len = prompt_len = None
+    if bias_token is not None and bias_token.numel() == 0:   # .. and no biases)
+        bias_cu = bias_token = bias_value = None
     m = 0 if bias_token is None else bias_token.numel()
     return _pass("logits_process", lib().sonic_logits_process, stream, (B, n, int(max_nodes), V), [
         ("logits", logits, logits.dtype, None), _number(int(logits.dtype is _BF16)), *_sized("plan", plan),
@@ -592,6 +596,8 @@ def cache_append(new_cu, k_new, v_new, k_cache, v_cache, cache_row_off, cache_ro
     select_len int32 [B]; bf16 rows, or codes with scales."""
     N, Hkv, d = k_new.shape
     B, rows = new_cu.numel() - 1, k_cache.shape[0]
+    if N == 0:   # (an empty tensor has no address; there is nothing to select)
+        select = select_len = None
     k, ks, v, vs = _planes(rows, Hkv, d, k_cache, k_scale, v_cache, v_scale)
     return _pass("cache_append", lib().sonic_cache_append, stream, (B, N, int(max_rows), Hkv, d), [
         ("new_cu", new_cu, _I32, None), ("select", select, _I32, (N,)), ("select_len", select_len, _I32, (B,)),

@@ -8,7 +8,7 @@ import workloads as W
 from oracle import tree as OT
 from oracle.attention import bf16_bits_to_f64
 from paper_2601_21927_amd import sonic
-from paper_2601_21927_amd.runner import DraftStep
+from paper_2601_21927_amd.runner import CompactCache, DraftStep
 from tests import gpu_helpers as H
 from tests.test_gpu_q4 import i32
 from tests.test_gpu_tree import tree
@@ -258,3 +258,42 @@ def test_many_biases_and_histories_without_a_prompt():
         c.run().check()
         c.prompt[:] = c.len
         c.run(out=False).check()
+
+
+def test_histories_and_biases_without_an_entry():
+    """Empty tensors, as a batch has them in which no request has any: as if they were left out."""
+    H.need_gpu()
+    c = Call(np.random.default_rng(19), 3, 500, hist=0, biases=0, parts=("penalties", "path"))
+    c.run().check()
+    want = c.out.clone()
+    none, zeros = i32([]), i32([0, 0, 0])
+    c.tokens, c.len, c.prompt = np.zeros(0, np.int32), np.zeros(3, np.int32), np.zeros(3, np.int32)
+    c.bias_cu, c.bias_token, c.bias_value = np.zeros(4, np.int32), np.zeros(0, np.int32), np.zeros(0, np.float32)
+    c.parts |= {"history", "biases"}
+    c.run()
+    assert torch.equal(c.out, want) and int(c.status.item()) == 0
+    assert none.data_ptr() == 0 and zeros.data_ptr() != 0
+
+
+def test_a_step_without_nodes():
+    """Room for nodes but none, and no room at all: every call returns, nothing is written."""
+    H.need_gpu()
+    for n in (0, 4):
+        status, step = i32([0]), DraftStep(2, n, 4)
+        cu, tokens = i32([0, 0, 0]), i32([5] * n)
+        x = torch.full((n, 100), 3.0, device="cuda")
+        assert step.plan_trees(cu, tokens, status) == sonic.OK
+        assert step.logits(x, status, node_token=tokens) == sonic.OK
+        assert step.accept(tokens, tokens, status) == sonic.OK
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0 and step.path_len.tolist() == [0, 0] and step.next_token.tolist() == [-1, -1]
+        assert torch.all(step.best == 0)
+        c = CompactCache(8, 2, 64, [0, 4], [4, 4], "cuda")
+        c.length.copy_(i32([3, 4]))
+        k = torch.zeros((n, 2, 64), dtype=torch.bfloat16, device="cuda")
+        q = torch.zeros((n, 4, 64), dtype=torch.bfloat16, device="cuda")
+        out = torch.full((n, 4, 64), 7.0, device="cuda")
+        assert c.tree_decode(step.plan, q, k, k, out, status, 4, 4) == sonic.OK
+        assert c.append(cu, k, k, status, 4, select=step.path, select_len=step.path_len) == sonic.OK
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0 and c.length.tolist() == [3, 4] and torch.all(out == 7.0)
