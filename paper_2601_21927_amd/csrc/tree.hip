@@ -933,7 +933,8 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeCall c, Tre
   const TreeReq r = tree_request(c, b);
   const int blocks = (r.len + kTreeBlock - 1) / kTreeBlock + (r.nodes + kTreeBlock - 1) / kTreeBlock;
   if (blockIdx.x * (SLOTS / sh.groups) >= r.nodes * G || r.len < 0 || r.len > c.max_ctx || blocks <= sh.range) return;
-  const int splits = (blocks + sh.range - 1) / sh.range;
+  // (nobody writes the places of rows past the request's last: a thread that stands there has no ranges, whatever they hold)
+  const int splits = row < r.nodes * G ? (blocks + sh.range - 1) / sh.range : 0;
   float M = -INFINITY, L = 0.f;
   bool odd = false, stopped = false;
   f32x4 A = {0.f, 0.f, 0.f, 0.f};
