@@ -55,7 +55,8 @@
  *   receives it returns without writing its outputs, so an error is sticky until
  *   the caller clears it.  The one exception is a pending SONIC_ERR_CAPACITY in
  *   the decode calls and those of a step over drafted tokens, where capacity is a
- *   per-request matter (see sonic_compressed_decode).
+ *   per-request matter (see sonic_compressed_decode).  In a step's calls any other
+ *   error takes its place, since they would go on behind it.
  * - softmax_scale: 0 selects the standard scale 1/sqrt(head_dim); any other value
  *   must be finite and positive.
  * - Setting the environment variable SONIC_DEBUG_SYNC=1 makes each GPU call
@@ -626,8 +627,8 @@ int32_t sonic_cache_evict(int32_t batch, int32_t max_rows, int32_t num_kv_heads,
  *
  * Nodes are packed over the batch: request b's are cu_nodes[b] .. cu_nodes[b+1]-1.  total_nodes is a host bound,
  * cu_nodes[B] <= total_nodes, so that a captured step serves trees of other sizes; rows of an output past cu_nodes[B]
- * are left as they were.  In all of these calls a pending SONIC_ERR_CAPACITY stops nothing; any other pending error
- * stops the call: nothing is written.
+ * are left as they were.  In all of these calls a pending SONIC_ERR_CAPACITY stops nothing, and gives way to any other error
+ * that one of them finds, then or in the same call; any other pending error stops the call: nothing is written.
  */
 
 /* Bytes of a plan (0 for negative sizes). */

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kLengthThreads) void append_lengths_kernel(AppendCa
     const uint64_t any = __ballot(bad) >> (threadIdx.x % kWave / kLengthLanes * kLengthLanes);
     if ((any & ((1u << kLengthLanes) - 1)) != 0) code = SONIC_ERR_BAD_LAYOUT;
     if (lane == 0 && b < c.batch && s_go) {
-      if (code != 0) raise_status(c.status, code);
+      if (code != 0) raise_step_status(c.status, code);
       else c.cache_len[b] = r.len + r.rows;
     }
   }

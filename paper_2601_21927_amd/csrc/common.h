@@ -41,6 +41,12 @@ __device__ __forceinline__ bool step_stops(const int32_t *status) {
   return pending != 0 && pending != SONIC_ERR_CAPACITY;
 }
 
+// What is wrong with a request of such a call.  A pending capacity error gives way to any other: the step goes on behind
+// it, and the other one would be lost.
+__device__ __forceinline__ void raise_step_status(int32_t *status, int32_t code) {
+  if (atomicCAS(status, 0, code) == SONIC_ERR_CAPACITY && code != SONIC_ERR_CAPACITY) atomicCAS(status, SONIC_ERR_CAPACITY, code);
+}
+
 // s_waitcnt vmcnt(N), the other counters left at their maximum (gfx9 encoding):
 // wait until at most N of this wave's vector-memory operations are outstanding.
 // They complete in issue order, so this waits for all but the N most recent.

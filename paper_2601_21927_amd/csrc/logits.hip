@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kWave) void logits_best_kernel(LogitsCall c, int pi
   LogitsReq r;
   const bool good = logits_request(c, b, &r);
   if (!good) {
-    if (row == 0 && lane == 0) raise_status(c.status, SONIC_ERR_BAD_LAYOUT);
+    if (row == 0 && lane == 0) raise_step_status(c.status, SONIC_ERR_BAD_LAYOUT);
     return;
   }
   if (row >= r.rows) return;

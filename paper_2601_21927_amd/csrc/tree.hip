@@ -61,7 +61,7 @@ __global__ __launch_bounds__(WAVE ? kWave : kMaxNodes) void tree_plan_kernel(con
   if (any & 2) return;
   if (any & 1) {
     if (i == 0) {
-      raise_status(status, SONIC_ERR_BAD_LAYOUT);
+      raise_step_status(status, SONIC_ERR_BAD_LAYOUT);
       req[b] = int2{0, 0};
     }
     return;
