@@ -725,10 +725,11 @@ int32_t sonic_logits_process(int32_t batch, int32_t total_rows, int32_t max_node
  *   parent          as for the plan (NULL: chains)
  *   node_token      device int32 [total_nodes]: the nodes' tokens
  *   chosen          device int32 [total_nodes]: for every node the token that follows it (sonic_logits_process's best, or
- *                   a sampler's)
+ *                   a sampler's); a negative one (best's -1: nothing was allowed) confirms no child
  *   path            device int32 [total_nodes]: request b's path, places in the request, at cu_nodes[b] ..; -1 behind it
  *   path_len        device int32 [B]: nodes of the path, 0 for a request without nodes
- *   next_token      device int32 [B]: chosen[the path's last node], the first token of the next step; -1 without nodes
+ *   next_token      device int32 [B]: chosen[the path's last node], the first token of the next step (negative, with a
+ *                   path_len of 1 or more, where nothing was allowed behind the path); -1 without nodes
  *   tokens ..       NULL, all four, or the requests' histories (as for sonic_logits_process), of which request b owns
  *                   token_cap[b] places: the path's tokens are added and token_len[b] is advanced
  *   dev_status      SONIC_ERR_CAPACITY when a history has no room for the path: the request's path_len is 0, its

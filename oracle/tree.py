@@ -33,12 +33,12 @@ def attend(q, k, v, k_new, v_new, parent, scale=None):
 
 
 def accepted(parent, token, chosen):
-    """(path, the token after it) from node 0 on; ([], -1) without nodes."""
+    """(path, the token after it) from node 0 on; ([], -1) without nodes.  A negative choice is no token."""
     if len(parent) == 0:
         return [], -1
     path = [0]
     while True:
-        step = [j for j in range(len(parent)) if parent[j] == path[-1] and token[j] == chosen[path[-1]]]
+        step = [j for j in range(len(parent)) if parent[j] == path[-1] and token[j] == chosen[path[-1]] >= 0]
         if not step:
             return path, int(chosen[path[-1]])
         path.append(step[0])

@@ -1059,7 +1059,8 @@ hipError_t launch_tree(const TreeCall &c, const TreeShape &sh, float *part, int 
 
 // ------------------------------------------------------------------ the path that is kept
 // One wave per request.  From node 0 on: of the nodes behind the present one whose parent it is and whose token is the one
-// chosen there, the lowest; until there is none.  Lane l looks at nodes l, l + 64, ..: a step is a few ballots.  Bound by the
+// chosen there, the lowest; until there is none (a negative choice, as the logits' call makes where nothing is allowed, is no
+// token, whatever a padded tree holds).  Lane l looks at nodes l, l + 64, ..: a step is a few ballots.  Bound by the
 // round trips before them and the stores behind: 4.3 us for eight trees of 32.
 __global__ __launch_bounds__(kWave) void tree_accept_kernel(TreePlan plan, const int32_t *__restrict__ parent, const int32_t *__restrict__ node_token,
                                                             const int32_t *__restrict__ chosen, int32_t *__restrict__ path,
@@ -1095,7 +1096,7 @@ __global__ __launch_bounds__(kWave) void tree_accept_kernel(TreePlan plan, const
     int found = -1;
 #pragma unroll
     for (int k = PER - 1; k >= 0; --k) {
-      const uint64_t m = __ballot(up[k] == now && token[k] == want && k * kWave + lane > now);
+      const uint64_t m = __ballot(want >= 0 && up[k] == now && token[k] == want && k * kWave + lane > now);
       if (m != 0) found = k * kWave + __builtin_ctzll(m);
     }
     now = found;

@@ -80,3 +80,48 @@ def test_too_many_rows_behind_a_capacity_error_and_capacity_behind_others():
         c.dev.row_cap.copy_(i32([1, 1]))
         assert c.dev.append(i32([0, 1, 4]), x, x, c.status, 3) == sonic.OK
         assert int(c.status.item()) == code
+
+
+def test_a_dead_end_confirms_no_padding():
+    """A row whose mask leaves nothing has -1 for its best token, and trees may be padded with nodes of token -1: the path ends
+    there, and neither the history nor the cache gets a padding row."""
+    H.need_gpu()
+    status = i32([0])
+    nodes, V = [4, 3, 70], 40
+    cu = np.concatenate([[0], np.cumsum(nodes)]).astype(np.int32)
+    n = int(cu[-1])
+    parents = [[-1, 0, 1, 1], [-1, 0, 1], [-1] + list(range(69))]
+    token = np.full(n, -1)                                    # all padding, but for ..
+    token[:2], token[4:6], token[7] = (5, 9), (3, 6), 8       # .. 5 -> 9; 3 -> 6; 8
+    logits = torch.zeros((n, V), device="cuda")
+    logits[0, 9] = logits[4, 6] = logits[5, 2] = 1.0
+    allowed = np.zeros((n, 64), np.uint8)
+    allowed[:, :V] = 1
+    allowed[1] = allowed[7] = 0                               # nothing behind 9, nothing behind 8
+    allowed = torch.from_numpy(np.packbits(allowed, axis=1, bitorder="little").view(np.int32)).cuda()
+    step = DraftStep(3, n, 70)
+    parent = i32(np.concatenate(parents))
+    assert step.plan_trees(i32(cu), parent, status) == sonic.OK
+    assert step.logits(logits, status, allowed=allowed) == sonic.OK
+    assert step.best[[0, 1, 4, 5, 7]].tolist() == [9, -1, 6, 2, -1]
+    history = dict(tokens=i32([0] * 300), token_off=torch.tensor([0, 100, 200], device="cuda"), token_cap=i32([100] * 3), token_len=i32([4] * 3))
+    assert step.accept(parent, i32(token), status, **history) == sonic.OK
+    c = Cache(np.random.default_rng(6), [10, 20, 30], 70, 2, 64, False)
+    x = bf16_to_device(normal_bits(np.random.default_rng(7), n, 2, 64))
+    assert c.dev.append(i32(cu), x, x, status, 70, select=step.path, select_len=step.path_len) == sonic.OK
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    assert step.path_len.tolist() == [2, 2, 1] and step.next_token.tolist() == [-1, 2, -1]
+    assert step.path[:7].tolist() == [0, 1, -1, -1, 0, 1, -1] and step.path[7:].tolist() == [0] + [-1] * 69
+    assert history["token_len"].tolist() == [6, 6, 5] and c.dev.length.tolist() == [12, 22, 31]
+    assert history["tokens"].tolist()[4:7] == [5, 9, 0] and history["tokens"].tolist()[204:206] == [8, 0]
+
+
+@pytest.mark.parametrize("choice", [-1, -2, -2 ** 31])
+def test_negative_choices_of_a_sampler(choice):
+    """.. end the path too, and are what the caller is given back."""
+    H.need_gpu()
+    status, step = i32([0]), DraftStep(1, 3, 3)
+    assert step.plan_trees(i32([0, 3]), None, status) == sonic.OK
+    assert step.accept(None, i32([1, choice, choice]), status, chosen=i32([choice] * 3)) == sonic.OK
+    assert step.path_len.tolist() == [1] and step.next_token.tolist() == [choice] and step.path.tolist() == [0, -1, -1]
