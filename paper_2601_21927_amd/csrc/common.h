@@ -312,7 +312,7 @@ struct TreeShape {
   int columns;        // q rows of a workgroup, in blocks of 16
   int waves;          // of a workgroup
   int tiles;          // of them in the largest request
-  int splits;         // ranges of a request of max_ctx rows
+  int splits;         // ranges of a request of max_ctx rows; 1 for more than 32 q rows
   int range;          // 32-row blocks of a range
   int run_log2;       // that many kv-heads of a range (2^) are neighbours on one XCD
   int groups;         // threads that share a row's ranges when they are joined

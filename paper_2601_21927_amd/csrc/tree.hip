@@ -442,7 +442,7 @@ __device__ __forceinline__ bool tree_finish(TreeColumns<D, CT, PARTS> &cols, con
   if (odd && !careful) return true;
 #pragma unroll
   for (int t = 0; t < CT; ++t) {
-    const int cc = 16 * t + col, row = row0 + cc;   // (acc and acc_stat are the wave's columns')
+    const int cc = 16 * t + col, row = row0 + cc;
     if (row >= rows || kg * MINE >= DB) continue;
     if (whole) {
       const int i = row / G;
@@ -464,10 +464,10 @@ __device__ __forceinline__ bool tree_finish(TreeColumns<D, CT, PARTS> &cols, con
 
 // What the workgroups of an attention call start with: its place in the call, the request, and what there is to do.
 struct TreePlace {
-  int kvh, rt, split, rows, cached, blocks, first, last;
-  bool whole;
+  int kvh, rt, split, rows, cached, blocks, first, last;   // (split, first, last: of a tile of up to 32 rows)
+  bool whole;        // the request is one range
   TreeReq r;
-  float *acc;        // the range's partial: the values, ..
+  float *acc;        // else the range's partial: the values, ..
   float2 *stat;      // .. and (max, sum), of COLS columns
 };
 // False: nothing to do.  The row tiles of one range are neighbours on one XCD (workgroup i goes to XCD i % 8): its rows come
@@ -475,13 +475,14 @@ struct TreePlace {
 template <int D, int COLS>
 __device__ __forceinline__ bool tree_begin(const TreeCall &c, const TreeShape &sh, float *part, int Hkv, int G, TreePlace *p) {
   __shared__ int s_stop;
-  const unsigned turn = blockIdx.x / kNumXcd, xcd = blockIdx.x % kNumXcd;
+  constexpr bool RANGES = COLS <= 32;   // (tiles of more rows are not cut: see tree_shape)
+  const unsigned turn = blockIdx.x / kNumXcd, xcd = blockIdx.x % kNumXcd, splits = RANGES ? sh.splits : 1;
   const unsigned at = turn / sh.tiles, unit = ((((at >> sh.run_log2) * kNumXcd + xcd) << sh.run_log2) + (at & ((1u << sh.run_log2) - 1)));
-  if (unit >= static_cast<unsigned>(c.batch) * Hkv * sh.splits) return false;
+  if (unit >= static_cast<unsigned>(c.batch) * Hkv * splits) return false;
   p->rt = turn % sh.tiles;
   p->kvh = unit % Hkv;
-  p->split = unit / Hkv % sh.splits;
-  const int b = unit / Hkv / sh.splits;
+  p->split = unit / Hkv % splits;
+  const int b = unit / Hkv / splits;
   if (threadIdx.x == 0) s_stop = step_stops(c.status);   // one look for the workgroup
   p->r = tree_request(c, b);
   __syncthreads();
@@ -494,6 +495,10 @@ __device__ __forceinline__ bool tree_begin(const TreeCall &c, const TreeShape &s
   }
   p->cached = (p->r.len + kTreeBlock - 1) / kTreeBlock;  // blocks of the cache, then of the nodes
   p->blocks = p->cached + (p->r.nodes + kTreeBlock - 1) / kTreeBlock;
+  p->first = 0, p->last = p->blocks;
+  p->whole = true;
+  p->acc = nullptr, p->stat = nullptr;
+  if constexpr (!RANGES) return !stop;
   p->first = p->split * sh.range;
   p->last = min(p->blocks, p->first + sh.range);
   if (p->first >= p->blocks) return false;
@@ -741,7 +746,7 @@ again:
 // behind the scores, with K a step further ahead, left the waves less room (64 requests of 180 .. 4,300 rows: 115 us, this
 // way 109).  4-bit rows are decoded on the way: the codes of a step ahead wait in registers, one quantisation block a lane.
 template <int D, int RW, int NW, bool Q4, int PARTS>
-__global__ __launch_bounds__(NW *kWave, 2) void tree_wide_kernel(TreeCall c, TreeShape sh, float *__restrict__ part, int Hkv, int G) {
+__global__ __launch_bounds__(NW *kWave, 2) void tree_wide_kernel(TreeCall c, TreeShape sh, int Hkv, int G) {
   typedef TreeColumns<D, 2, PARTS> Columns;
   constexpr int CT = 2, KS = D / 32, DB = D / 16, DC = D / 8, BR = kTreeBlock;
   constexpr int KW = NW / RW, SB = NW / 2, NB = SB / KW;   // key groups; blocks of a step, and of them a wave's
@@ -754,9 +759,9 @@ __global__ __launch_bounds__(NW *kWave, 2) void tree_wide_kernel(TreeCall c, Tre
   __shared__ __align__(16) uint16_t lds[4 * SB * TILE];   // K of two steps, V of two steps
   __shared__ float2 stat[NW * 32];
   TreePlace p;
-  if (!tree_begin<D, COLS>(c, sh, part, Hkv, G, &p)) return;
+  if (!tree_begin<D, COLS>(c, sh, nullptr, Hkv, G, &p)) return;
   const TreeReq &r = p.r;
-  const int cached = p.cached, blocks = p.blocks, first = p.first, kvh = p.kvh;   // (a range is whole steps)
+  const int cached = p.cached, blocks = p.blocks, kvh = p.kvh;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int rg = wave % RW, kg = wave / RW;
   const int col = lane & 15, quarter = lane >> 4;
@@ -770,7 +775,7 @@ __global__ __launch_bounds__(NW *kWave, 2) void tree_wide_kernel(TreeCall c, Tre
   const uint16_t *knew = c.k_new + static_cast<size_t>(r.first) * row_elems + kvh * D;
   const uint16_t *vnew = c.v_new + static_cast<size_t>(r.first) * row_elems + kvh * D;
   uint16_t *const kbuf = lds, *const vbuf = lds + 2 * SB * TILE;   // [2 steps][SB blocks][32 rows][D]
-  const int steps = (p.last - first + SB - 1) / SB;
+  const int steps = (blocks + SB - 1) / SB;
   const int full = r.len / BR;                       // blocks without a row that some column does not see
   bool careful = false, odd = false;
 
@@ -782,7 +787,7 @@ __global__ __launch_bounds__(NW *kWave, 2) void tree_wide_kernel(TreeCall c, Tre
 #pragma unroll
     for (int n = 0; n < NB; ++n) cols.scores(kt + (KW * n + kg) * TILE, qf, col, quarter, s[n]);
     order_operands<NB * 2 * KS, 1, CT, kAheadK>();
-    const int g = first + SB * step + kg;
+    const int g = SB * step + kg;
     if (__builtin_expect(g + KW * (NB - 1) >= full, 0))
 #pragma unroll
       for (int n = 0; n < NB; ++n) tree_mask<CT>(c, r, g + KW * n, cached, node, quarter, s[n]);
@@ -806,7 +811,7 @@ again:
     const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint16_t *)lds)) +
                         wave * NJ * kWave * 16;
     auto issue = [&](int step, const uint16_t *cache, const uint16_t *fresh, uint32_t to, bool is_v) {
-      const int g = min(first + SB * step + wave * NJ / NI, blocks - 1);
+      const int g = min(SB * step + wave * NJ / NI, blocks - 1);
       const int r0 = (g < cached ? g : g - cached) * BR;
       const int left = (g < cached ? r.len : r.nodes) - r0;
       const char *src = reinterpret_cast<const char *>(g < cached ? cache : fresh) + static_cast<size_t>(r0) * row_bytes;
@@ -840,7 +845,7 @@ again:
     struct Raw { u32x4 c; uint32_t s; };
     auto fetch = [&](int step, const void *codes, const uint8_t *scales, const uint16_t *fresh) {
       Raw x;
-      const int g = min(first + SB * step + row / BR, blocks - 1);
+      const int g = min(SB * step + row / BR, blocks - 1);
       if (g < cached) {
         const size_t at = min(g * BR + row % BR, r.len - 1);
         x.c = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(codes) + code0 + at * row_codes);
@@ -892,8 +897,8 @@ again:
     }
   }
 
-  if (tree_finish<D, CT, PARTS, RW, KW>(cols, c, r, reinterpret_cast<f32x4 *>(lds), stat, wave, lane, row0, p.rows, Hkv, G, kvh, p.whole, careful,
-                                        odd, p.acc + 32 * rg * D, p.stat + 32 * rg)) {
+  if (tree_finish<D, CT, PARTS, RW, KW>(cols, c, r, reinterpret_cast<f32x4 *>(lds), stat, wave, lane, row0, p.rows, Hkv, G, kvh, true, careful,
+                                        odd, nullptr, nullptr)) {
     careful = true;   // once more, the nodes' V with a look
     __syncthreads();
     goto again;
@@ -1006,8 +1011,9 @@ TreeShape tree_shape(int batch, int Hkv, int G, int D, int max_nodes, int max_ct
   while (sh.columns < 8 && 16 * sh.columns < rows && pairs * tiles(sh.columns) > 256) sh.columns *= 2;
   sh.tiles = static_cast<int>(tiles(sh.columns));
   const long units = pairs * sh.tiles;
-  const long splits = std::max(1L, std::min(256 / units, blocks / (units >= 128 ? 32 : 16)));
-  sh.range = static_cast<int>((blocks + splits - 1) / splits + 3) / 4 * 4;   // whole steps
+  // (tiles of more than 32 rows are taken where half as large ones were more than 256, so they are 129 and more)
+  const long splits = sh.columns > 2 ? 1 : std::max(1L, std::min(256 / units, blocks / (units >= 128 ? 32 : 16)));
+  sh.range = static_cast<int>((blocks + splits - 1) / splits + 3) / 4 * 4;   // four waves' turns
   sh.splits = static_cast<int>((blocks + sh.range - 1) / sh.range);
   sh.waves = units * sh.splits <= 256 && (sh.columns > 2 || sh.range > (q4 ? 32 : 96)) ? 8 : 4;
   for (sh.run_log2 = 0; q4 && sh.run_log2 < 3 && Hkv % (2 << sh.run_log2) == 0; ++sh.run_log2) {
@@ -1026,10 +1032,10 @@ static void launch_tree_rows(const TreeCall &c, const TreeShape &sh, float *part
   else if (sh.columns == 1) tree_kernel<D, 1, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
   else if (sh.columns == 2 && sh.waves == 8) tree_kernel<D, 2, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, part, Hkv, G);
   else if (sh.columns == 2) tree_kernel<D, 2, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
-  else if (sh.columns == 4 && sh.waves == 8) tree_wide_kernel<D, 2, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, part, Hkv, G);
-  else if (sh.columns == 4) tree_wide_kernel<D, 2, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
-  else if (sh.waves == 8) tree_wide_kernel<D, 4, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, part, Hkv, G);
-  else tree_wide_kernel<D, 4, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, part, Hkv, G);
+  else if (sh.columns == 4 && sh.waves == 8) tree_wide_kernel<D, 2, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, Hkv, G);
+  else if (sh.columns == 4) tree_wide_kernel<D, 2, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, Hkv, G);
+  else if (sh.waves == 8) tree_wide_kernel<D, 4, 8, Q4, PARTS><<<grid, more, 0, stream>>>(c, sh, Hkv, G);
+  else tree_wide_kernel<D, 4, 4, Q4, PARTS><<<grid, block, 0, stream>>>(c, sh, Hkv, G);
 }
 
 template <int D>
