@@ -125,3 +125,66 @@ def test_negative_choices_of_a_sampler(choice):
     assert step.plan_trees(i32([0, 3]), None, status) == sonic.OK
     assert step.accept(None, i32([1, choice, choice]), status, chosen=i32([choice] * 3)) == sonic.OK
     assert step.path_len.tolist() == [1] and step.next_token.tolist() == [choice] and step.path.tolist() == [0, -1, -1]
+
+
+@pytest.mark.parametrize("nodes", [4, 100])
+@pytest.mark.parametrize("cu,parent,most,rows", [([1, 2, 4], [-1] * 4, 4, slice(0, 2)), ([0, 2, 5], [-1] * 4, 4, slice(2, 4)),
+                                                 ([0, 3, 4], [-1] * 4, 2, slice(0, 2)), ([0, 2, 4], [-1, 1, -1, 0], 4, slice(0, 2)),
+                                                 ([0, 2, 4], [-1, 0, -2, 0], 4, slice(2, 4)), ([0, 2, 4], [-1, 0, -1, 7], 4, slice(2, 4))])
+def test_a_request_with_a_malformed_tree_has_no_rows(cu, parent, most, rows, nodes):
+    """.. whatever its caller does about the status word: attention, best tokens and path leave its rows as they were."""
+    H.need_gpu()
+    nodes = most if most < 4 else nodes
+    c = Cache(np.random.default_rng(3), [30, 300], 1, 2, 64, False)
+    step = DraftStep(2, 4, nodes)
+    whole = step.plan_trees(i32([0, 2, 4]), None, c.status)            # an earlier step's plan
+    assert whole == sonic.OK and step.plan_trees(i32(cu), i32(parent), c.status) == sonic.OK
+    assert int(c.status.item()) == sonic.ERR_BAD_LAYOUT
+    c.status.zero_()
+    q, x = (torch.zeros((4, h, 64), dtype=torch.bfloat16, device="cuda") for h in (4, 2))
+    out, best = torch.full((4, 4, 64), 7.0, device="cuda"), torch.full((4,), -7, dtype=torch.int32, device="cuda")
+    assert c.dev.tree_decode(step.plan, q, x, x, out, c.status, nodes, 300) == sonic.OK
+    step.best.fill_(-7)
+    step.path.fill_(-9)
+    assert step.logits(torch.zeros((4, 50), device="cuda"), c.status) == sonic.OK
+    assert step.accept(i32(parent), best, c.status) == sonic.OK
+    torch.cuda.synchronize()
+    assert torch.all(out[rows] == 7.0) and torch.all(step.best[rows] == -7) and torch.all(step.path[rows] == -9)
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_a_cache_without_room_is_brought_up_to_its_history(q4):
+    """A path that its history had room for and one cache had not: that cache alone stays behind, its rows are told by the lengths,
+    and a later append of that request's path alone brings it up."""
+    H.need_gpu()
+    rng = np.random.default_rng(8)
+    nodes = [3, 4, 2]
+    cu = np.concatenate([[0], np.cumsum(nodes)]).astype(np.int32)
+    caches = [Cache(rng, [10, 20, 30], 4, 2, 64, q4) for _ in range(2)]
+    caches[1].dev.row_cap[1] = 21                             # of the second layer, request 1: one row left
+    status, step = i32([0]), DraftStep(3, 9, 4)
+    bits = [[normal_bits(rng, 9, 2, 64) for _ in range(2)] for _ in caches]
+    history = dict(tokens=i32([0] * 60), token_off=torch.tensor([0, 20, 40], device="cuda"), token_cap=i32([20] * 3), token_len=i32([10] * 3))
+    before = [c.dev.length.clone() for c in caches]
+    rows = [rows_of(c) for c in caches]
+    assert step.plan_trees(i32(cu), None, status) == sonic.OK
+    assert step.accept(None, i32([5] * 9), status, chosen=i32([5, 5, 0, 5, 5, 5, 0, 0, 0]), **history) == sonic.OK
+    for c, x in zip(caches, bits):
+        assert c.dev.append(i32(cu), *(bf16_to_device(y) for y in x), status, 4, select=step.path, select_len=step.path_len) == sonic.OK
+    assert int(status.item()) == sonic.ERR_CAPACITY
+    assert step.path_len.tolist() == [3, 4, 1] and history["token_len"].tolist() == [13, 14, 11]
+    assert caches[0].dev.length.tolist() == [13, 24, 31] and caches[1].dev.length.tolist() == [13, 20, 31]
+    # with room, the path of the requests that stayed behind, and of no other
+    status.zero_()
+    caches[1].dev.row_cap[1] = 24
+    for c, x, n in zip(caches, bits, before):
+        behind = torch.where(c.dev.length == n, step.path_len, 0).int()
+        assert c.dev.append(i32(cu), *(bf16_to_device(y) for y in x), status, 4, select=step.path, select_len=behind) == sonic.OK
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    for c, x, r in zip(caches, bits, rows):
+        assert c.dev.length.tolist() == [13, 24, 31]
+        for b, m in enumerate([3, 4, 1]):
+            for j in range(m):
+                put(c, r, int(c.off[b] + c.lens[b]) + j, [y[cu[b] + j] for y in x])
+        assert all(np.array_equal(a, b) for a, b in zip(rows_of(c), r))
