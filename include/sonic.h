@@ -742,7 +742,9 @@ int32_t sonic_tree_accept(int32_t batch, int32_t total_nodes, int32_t max_nodes,
 
 /*
  * New rows to the end of every request's cache: cache row cache_row_off[b] + cache_len[b] + j takes new row
- * new_cu[b] + select[new_cu[b] + j], for j < select_len[b], and cache_len[b] is advanced by that many.
+ * new_cu[b] + select[new_cu[b] + j], for j < select_len[b], and cache_len[b] is advanced by that many.  A step adds nothing to
+ * row weights, and this call does not know of them (nor of keep_idx): before the next sonic_cache_evict or
+ * sonic_compressed_decode_weighted the caller sets those of the rows from the old cache_len[b] on, which hold what they held.
  *   max_rows        host bound on the rows appended to a request
  *   new_cu          device int32 [B+1], non-decreasing, new_cu[B] <= total_new: request b's new rows
  *   select          NULL together with select_len: all of them, in order; or device int32 [total_new] and [B]

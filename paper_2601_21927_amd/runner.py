@@ -217,7 +217,8 @@ class CompactCache:
 
     def append(self, new_cu, k_new, v_new, status, max_rows: int, select=None, select_len=None, stream=None) -> int:
         """New rows to the end of the cache: all of a request's, or those at select.  row_weight and keep_idx of the rows are
-        the caller's to set."""
+        the caller's to set before the next evict or decode_weighted: they hold what a dropped row left there.  With `old` the
+        lengths before and `request` each row's request, the new rows are (place >= old[request]) & (place < length[request])."""
         return sonic.cache_append(new_cu, k_new, v_new, self.k, self.v, self.row_off, self.row_cap, self.length, status, max_rows,
                                   select=select, select_len=select_len, stream=stream)
 
@@ -270,7 +271,7 @@ class Q4Cache:
 
     def append(self, new_cu, k_new, v_new, status, max_rows: int, select=None, select_len=None, stream=None) -> int:
         """New rows, rounded, to the end of the cache: all of a request's, or those at select.  row_weight and keep_idx of the
-        rows are the caller's to set."""
+        rows are the caller's to set, as in CompactCache.append."""
         return sonic.cache_append(new_cu, k_new, v_new, self.k, self.v, self.row_off, self.row_cap, self.length, status, max_rows,
                                   select=select, select_len=select_len, k_scale=self.k_scale, v_scale=self.v_scale, stream=stream)
 
