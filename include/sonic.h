@@ -625,6 +625,11 @@ int32_t sonic_cache_evict(int32_t batch, int32_t max_rows, int32_t num_kv_heads,
  * and needs no host round trip.  A chain of nodes is also a piece of a prompt taken over an existing cache:
  * sonic_tree_decode, then sonic_cache_append of all its rows.
  *
+ * Each call checks the room of what it writes and of nothing else.  A path may fit the history but not a cache, or one
+ * layer's cache and not another's: it is then in those that had room, SONIC_ERR_CAPACITY is raised, and cache_len tells which
+ * stayed as they were.  Give every cache of a request at least as much room as its history, or, with room made, append that
+ * path where it is missing (the same select, a select_len of 0 for the requests that have theirs) before the next step.
+ *
  * Nodes are packed over the batch: request b's are cu_nodes[b] .. cu_nodes[b+1]-1.  total_nodes is a host bound,
  * cu_nodes[B] <= total_nodes, so that a captured step serves trees of other sizes; rows of an output past cu_nodes[B]
  * are left as they were.  In all of these calls a pending SONIC_ERR_CAPACITY stops nothing, and gives way to any other error
@@ -643,8 +648,8 @@ size_t sonic_tree_plan_bytes(int32_t batch, int32_t total_nodes, int32_t max_nod
  *   plan          device, 256-byte aligned, >= sonic_tree_plan_bytes(B, total_nodes, max_nodes) bytes; the calls that
  *                 take it are given the same B, total_nodes and max_nodes
  *   dev_status    SONIC_ERR_BAD_LAYOUT for inconsistent cu_nodes, a request of more than max_nodes nodes, or a parent that
- *                 does not come before its node; such a request has no nodes in the plan, and the others' parts are not to be
- *                 relied on either
+ *                 does not come before its node; such a request (the only one, or the first to be found) has no nodes in
+ *                 the plan, and the others' parts are not to be relied on: the plan is made again
  * Returns SONIC_ERR_UNSUPPORTED for max_nodes > 256 and SONIC_ERR_WORKSPACE for a plan that is too small, as the calls that
  * take it do.
  */
