@@ -113,7 +113,8 @@ enum {
  * to 10 it rose with every entry point that was added as well.  Those of the last three sections (4-bit
  * rows, row weights and eviction, drafted tokens: sonic_kv_compact_q4 to sonic_cache_append) came to
  * version 10 without a new number: a program that was built before them runs unchanged, and one that
- * needs them looks for their names.
+ * needs them looks for their names.  So did two mends of the last section: a pending capacity error gives
+ * way to any other, and sonic_tree_accept takes a negative choice for none.
  */
 int32_t sonic_abi_version(void);
 
@@ -664,7 +665,9 @@ size_t sonic_tree_decode_workspace_bytes(int32_t batch, int32_t max_nodes, int32
  *     out[i][h] = softmax_r(scale * <q[i][h], k[r][g(h)]>) v[r][g(h)]
  * over the request's cache rows 0 .. cache_len[b] - 1 and the rows k_new, v_new of the nodes that i sees.  The cache is
  * only read: sonic_cache_append adds the rows that are kept.
- *   max_ctx         host bound, at most 2^30: cache_len[b] <= max_ctx for every b; 0 for empty caches
+ *   max_ctx         host bound, at most 2^30: cache_len[b] <= max_ctx for every b; 0 for empty caches.  The work of few
+ *                   requests is cut into ranges by it alone: far above the lengths it costs time (one request of 8,000 rows
+ *                   three times its own under a bound of 100,000), so capture a step for a few bounds
  *   k_cache, v_cache   device bf16 [rows][Hkv][d] with k_scale = v_scale = NULL, or 4-bit rows with their scales; then the
  *                   nodes' rows are rounded as sonic_cache_append would, and take part at their 4-bit values
  *   q               device bf16 [total_nodes][Hq][d];  k_new, v_new: device bf16 [total_nodes][Hkv][d]

@@ -13,7 +13,9 @@
 // K and V come by direct-to-LDS loads.  Up to 32 rows are one wave's columns, and the waves of a workgroup take blocks in
 // turn, each with LDS of its own (tree_kernel); of more rows, waves with 32 each share the blocks (tree_wide_kernel).
 // An fp32 output takes a probability in three bf16 values (2^-26 of it is left), a bf16 output in one: its rounding, with
-// the sum taken over the rounded ones, is of the size of the output's own (1.2 to 1.3 times that in all).
+// the sum taken over the rounded ones, is of the size of the output's own (1.2 to 1.3 times that in all).  Two would leave the
+// output's alone and cost nothing where HBM bounds the call, but trees of 32 over eight caches of 1,328 rows 20.0 us instead of
+// 17.7 and chains of 250 over four of 1,584 53 instead of 43; a caller who wants them takes fp32.
 // Ranges of a request are joined by another kernel.
 //
 // Bound by, trees of 32 over eight caches of 1,328 rows (32 / 8 heads of 128, bf16 out, 17.7 us; the bytes alone 9.5, the
@@ -990,15 +992,24 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeCall c, Tre
 //   16, tiles of 16 rows 14.5 us, of 32 17.0, of 64 in two ranges 21.9; trees of 32, tiles of 16 22.8, of 32 17.7, of 64 in two
 //   ranges 23.8, of 128 in four 24.0; 32 of 1,000 rows, trees of 32: tiles of 32 57, of 64 44, of 128 39).  Tiles of 16 rows
 //   use the matrix cores half, which long rows show (one request of 8,000 rows, trees of 64: 30.7 us and, of 32, 23.6), and
-//   4-bit rows are decoded once for each tile.
+//   4-bit rows are decoded once for each tile (one request of 100,001, trees of 13: 72.6 us, tiles of 16 rows 88; short ones
+//   would be better off with those: 8 of 1,328, trees of 16: 19.2 and 15.5).  4-bit rows in tiles of 128 rows of 128 values
+//   spill 2 to 15 registers, and are still better than tiles of 64, which spill none (64 requests of 1,500 rows, trees of 64: 129
+//   us, fp32 203; 175 and 242).
 // - Ranges: up to 256 workgroups, of 512 rows and more (1,024 from 128 tiles on: the join is a launch of 4 us).  One request
 //   of 8,000 rows, trees of 16: 4 ranges 20.8 us, 8 16.1, 16 18.0; 8 of 1,328 rows, trees of 8: one range 14.7, two 16.1.
+//   They are those of max_ctx rows, the lengths being on the device: one request of 8,000 rows takes 52 us under a bound of
+//   100,000, 15.9 under its own; 6,000 4-bit rows 49 and 16.1; eight of 1,328, trees of 32, 19.9 and 17.6.
 //   Uneven lengths are not evened out: 64 requests of 180 .. 4,300 rows, trees of up to 16, gained 5 to 8 us of 114 in three
 //   ranges or in ranges shared evenly over the batch, which cost 64 equal ones of 1,500 rows 85 us instead of 77.
 // - Eight waves where a CU has one workgroup: of up to 32 rows if it is long (4 requests of 7,552 rows, 28 / 4 heads, trees of
 //   61, fp32: 67 us, with four 73; one of 100,001 4-bit rows: 16 ranges of eight waves 73, 32 of four 74, and 16 of four 99),
 //   of more rows always (chains of 250 over four requests of 1,584 rows 42.6 and 49.9; trees of 64 over eight of 1,328 24.5
-//   and 27.6).  With two workgroups a CU four are better (64 requests of 1,500 rows, trees of 16: 78, with eight 84).
+//   and 27.6).  With two workgroups a CU four are better (64 requests of 1,500 rows, trees of 16: 78, with eight 84).  Short
+//   ranges are better off with four: trees of 32 over eight of 1,328 rows (44 blocks) 17.4 us, with eight 20.1; 32 of 800 4-bit
+//   rows (26 blocks), trees of 8, 16.2 and 17.3, of 1,300 (42) 20.5 and 20.5, of 2,000 (64) 25.3 and 25.1, trees of 4 22.4 and
+//   20.3.  For bf16 rows the border is between products and bytes rather than at a length: small trees, which HBM bounds, have
+//   four ahead by 0 to 5 % on both sides of it (32 of 2,900 rows, trees of 8: 71.1 and 72.7; of 4,500 104.5 and 107.5).
 // - Neighbours: lines of 4-bit rows hold several heads' codes and scales, so up to eight heads of a range go to one XCD, as
 //   long as every XCD still gets as many workgroups (64 requests of 1,500 rows, trees of 8: 39.0 us, each head on another XCD
 //   46.5; one of 100,001 rows: 114 MB fetched instead of 266, 70.6 us instead of 72).

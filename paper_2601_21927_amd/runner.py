@@ -212,7 +212,8 @@ class CompactCache:
                                                 self.row_weight, ws, status, max_ctx, stream=stream)
 
     def tree_decode(self, plan, q, k_new, v_new, out, status, max_nodes: int, max_ctx: int, stream=None) -> int:
-        """The attention of drafted tokens over the cache and their own paths; the cache stays as it is."""
+        """The attention of drafted tokens over the cache and their own paths; the cache stays as it is.  A cache's calls share
+        a workspace: side by side (on two streams, in two graphs) take sonic.tree_decode with one each."""
         return _tree_decode(self, plan, q, k_new, v_new, out, status, max_nodes, max_ctx, stream)
 
     def append(self, new_cu, k_new, v_new, status, max_rows: int, select=None, select_len=None, stream=None) -> int:
@@ -265,7 +266,7 @@ class Q4Cache:
 
     def tree_decode(self, plan, q, k_new, v_new, out, status, max_nodes: int, max_ctx: int, stream=None) -> int:
         """The attention of drafted tokens over the cache and their own paths, at the 4-bit values of their rows; the cache
-        stays as it is."""
+        stays as it is, and its calls share a workspace, as CompactCache's."""
         return _tree_decode(self, plan, q, k_new, v_new, out, status, max_nodes, max_ctx, stream, k_scale=self.k_scale,
                             v_scale=self.v_scale)
 
@@ -283,7 +284,7 @@ class Q4Cache:
 
 class DraftStep:
     """A step over drafted tokens of `batch` requests, up to total_nodes of them and max_nodes a request: what is made once
-    and used by every layer and every step (the plan, the confirmed paths, the logits' workspace).
+    and used by every layer and every step (the plan, the confirmed paths, the logits' workspace): one step at a time.
 
     plan_trees, then CompactCache.tree_decode (or Q4Cache's) per layer with `plan`, `logits`, `accept`, and the caches'
     append with path and path_len."""
